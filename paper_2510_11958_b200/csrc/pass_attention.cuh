@@ -44,18 +44,6 @@ constexpr int PK_PA_END = PK_PA_W + 2 * PK_D * 4 + (PK_D / 2) * 8;
 static_assert(PK_PA_TILES_END <= PK_PA_RED, "attention scratch overlaps");
 static_assert(PK_PA_END <= PK_SCRATCH_BYTES, "attention scratch does not fit");
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_wait_all() {
-  asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3)
-               : "r"(addr));
-}
-
 // Key slices of one (sequence, kv head): nsplit slices of CH cached keys; the last slice also
 // takes the R keys of the pass itself.
 __device__ __forceinline__ void attn_plan_device(const PassParams &P, int pos0, int &nsplit, int &CH) {

@@ -204,6 +204,117 @@ dmtd_status dmtd_attention_decode_static(const float *q, const void *k, const vo
                                          int32_t n_kv_heads, int32_t head_dim, int32_t max_seq,
                                          int32_t pos0, float *out, void *cuda_stream);
 
+/* ---- requests of unequal length: a paged KV cache -------------------------------------------
+ * The calls of a context advance equal sequences in lock-step; these three, which need no context,
+ * serve requests of unequal length that come and go.  Keys and values live in pages of a pool,
+ * page_size positions each; row b of a table names request b's pages in the order of positions.  A step is
+ *
+ *   dmtd_paged_plan        pages for the new tokens, a slot for each of them        once a step
+ *   dmtd_paged_append      QK-norm, rotary embedding, keys and values into slots    once a layer
+ *   dmtd_paged_attention   new rows against their request's pages                   once a layer
+ *
+ * (the paper's cyclical refilling, Section 2.2, with requests of their own lengths: one to tau new
+ * rows each, or a piece of a prompt).  (The paper has no counterpart: it measures static batches.)
+ * Lengths, tables and offsets are read on the device when the kernels run, so a captured graph of
+ * a step stays valid while requests grow.  Values in them that do not fit the buffers are cut off: lengths
+ * to [0, table_stride * page_size], row offsets to [0, n_rows]; slots and pages outside the
+ * pool are left out.  All pointers are device pointers on the current device, all arrays of
+ * the interface dense int32 unless a stride is given; calls are asynchronous on `cuda_stream`.
+ *
+ * The rows of a page of one kv head are head_dim dense values; strides count values, so that
+ * pools in the orders [page][kv head][row] and [page][row][kv head], or with K and V side by side,
+ * serve alike.  K and V have the same strides.  Rows begin on 16-byte boundaries. */
+typedef struct {
+  void *k, *v;                          /* device, `dtype`                                      */
+  int32_t dtype;                        /* DMTD_F32, DMTD_BF16 or DMTD_F16                      */
+  int32_t n_pages, page_size;           /* page_size: a power of two; at most 2^31 - 1 slots    */
+  int32_t n_kv_heads, head_dim;         /* head_dim 64 or 128                                   */
+  int64_t page_stride, head_stride, row_stride;
+} dmtd_paged_cache;
+
+#define DMTD_PAGED_MAX_REQUESTS 8192
+
+/* Pages and slots for a step's new tokens, from the requests' lengths.
+ *   lens [n_requests]         keys cached before the step
+ *   n_new [n_requests]        new tokens; 0: the request waits; negative: it has ended, and its
+ *                             pages go back to the pool before any are given out
+ *   table [n_requests][table_stride]   in place: entries of the pages given out are written, no others
+ *   free_pages [n_pages], n_free [1]   the pool's free pages as a stack of *n_free entries: pages are
+ *                             taken from its end, ended requests' pages (in the order of requests
+ *                             and of positions; ids outside the pool left out) are put there first
+ *   n_rows                    rows of the step's token arrays, the sum of the new tokens or more
+ * Out:
+ *   row_start [n_requests + 1]   rows of request b: [row_start[b], row_start[b + 1])
+ *   position, slot [n_rows]   of every row; slot = page * page_size + row of the page.  Rows without
+ *                             a slot (behind the last request, or of a refused one): slot -1, position 0
+ *   granted [n_requests]      n_new[b], or 0 if the request is refused or has ended
+ *   lens_out [n_requests]     lens + granted; 0 for ended requests.  May be lens
+ *   n_free_out [1]            entries left on the stack.  May be n_free
+ * Pages are given out in the order of requests.  A request is refused as a whole, and keeps what it
+ * has, if the stack does not hold all the pages that it and those in front of it ask for, if it would outgrow
+ * its table row, or if its rows do not end within n_rows.  Its rows keep their place.
+ * The arrays that are written must not overlap others but where it says so above.
+ * Errors: SHAPE if page_size is not a power of two; CAPACITY for more than DMTD_PAGED_MAX_REQUESTS
+ * requests, 2^31 - 1 slots, or 2^30 rows or table entries. */
+dmtd_status dmtd_paged_plan(const int32_t *lens, const int32_t *n_new, int32_t n_requests,
+                            int32_t page_size, int32_t *table, int32_t table_stride,
+                            int32_t *free_pages, int32_t n_pages, const int32_t *n_free,
+                            int32_t n_rows, int32_t *row_start, int32_t *position, int32_t *slot,
+                            int32_t *granted, int32_t *lens_out, int32_t *n_free_out,
+                            void *cuda_stream);
+
+/* Step a3 for new rows: RMSNorm of every query and key head (x / sqrt(mean x^2 + rms_eps) * norm),
+ * rotary embedding (pairs (i, i + head_dim / 2) turned by position * rope_theta^(-2i / head_dim)),
+ * keys and values rounded to the cache's type and written to their slots, queries to q_out.
+ *   q [n_rows][n_q_heads][head_dim], k, v [n_rows][n_kv_heads][head_dim]   in `dtype`, rows
+ *                             q_stride / k_stride / v_stride values apart (three parts of one
+ *                             projection's output, say), heads dense
+ *   q_norm, k_norm            float [head_dim], or NULL: no norm
+ *   rope_theta                0: no rotation
+ *   position, slot [n_rows]   rows whose slot is outside the pool are left alone, in the
+ *                             cache and in q_out.  Slots of a call are distinct: two rows with the
+ *                             same slot leave a mixture of their values there
+ *   q_out [n_rows][n_q_heads][head_dim]   in `dtype`; may be q where q is dense
+ * n_q_heads may be 0 (keys and values only).  Arithmetic is fp32 (angles: 64 bits), each result is rounded once.
+ * Errors: INVALID_ARG for rows that do not begin on 16-byte boundaries or strides shorter than a
+ * row; SHAPE for types and head_dim. */
+dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32_t dtype,
+                              int64_t q_stride, int64_t k_stride, int64_t v_stride, int32_t n_rows,
+                              int32_t n_q_heads, const float *q_norm, const float *k_norm,
+                              float rms_eps, float rope_theta, const int32_t *position,
+                              const int32_t *slot, const dmtd_paged_cache *cache, void *q_out,
+                              void *cuda_stream);
+
+/* dmtd_attention_decode for requests of unequal length over a paged cache.  Row r of request b's n
+ * new rows sits at position lens[b] - n + r and attends to positions [0, lens[b] - n + r] of that
+ * request; scores are scaled by 1 / sqrt(head_dim).
+ *   q [n_rows][n_q_heads][head_dim]   in q_dtype, rows q_stride values apart, heads dense, already
+ *                             normalised and rotated
+ *   row_start [n_requests + 1], rising; lens [n_requests]: keys, the new rows' own among them (which
+ *                             are in the cache already); table [n_requests][table_stride]
+ *   max_new                   the most new rows of a request as far as the host knows, 0 = unknown.
+ *                             Chooses between forms of the kernels; results do not hang on it
+ *   scratch                   device memory of at least DMTD_PAGED_ATTENTION_SCRATCH_BYTES bytes,
+ *                             16-byte aligned, owned by the caller; holds partial results while the call's
+ *                             kernels run (calls sharing one scratch must be stream-ordered, captured
+ *                             graphs among them).  Nothing in it needs to be cleared or kept
+ *   out [n_rows][n_q_heads][head_dim]   in q_dtype.  Rows of no request are left as they were
+ * Types: fp32 queries with any cache (results to fp32 accuracy: fp32 queries, and probabilities, enter
+ * the tensor cores as two or three 16-bit parts), or 16-bit queries with a cache of the same type (the probabilities
+ * are rounded once to that type before the product with V, sums and maxima are fp32).  A row that sees no key (a length below
+ * its rows, pages outside the pool, which take their keys out), or none whose weight is not zero, gives zeros.
+ * Keys and values of positions that a row does not see have no influence on it, whatever they hold.
+ * Errors: SHAPE for head_dim not 64/128, n_q_heads % n_kv_heads != 0 or more than 16 query heads per
+ * KV head; UNSUPPORTED for 16-bit queries and a cache of another type; INVALID_ARG for rows that do
+ * not begin on 16-byte boundaries or strides shorter than a row; CAPACITY if scratch_bytes is too small, or
+ * beyond DMTD_PAGED_MAX_REQUESTS requests, 2^31 - 1 positions to a table row, 2^24 query rows times heads. */
+#define DMTD_PAGED_ATTENTION_SCRATCH_BYTES (48u << 20)
+dmtd_status dmtd_paged_attention(const void *q, int32_t q_dtype, int64_t q_stride, int32_t n_rows,
+                                 int32_t n_q_heads, const int32_t *row_start, const int32_t *lens,
+                                 int32_t n_requests, const int32_t *table, int32_t table_stride,
+                                 int32_t max_new, const dmtd_paged_cache *cache, void *scratch,
+                                 size_t scratch_bytes, void *out, void *cuda_stream);
+
 /* Host-buffer forms of prefill and decode_cycle (same semantics; the copies to and from the
  * device are part of the call, which returns after the stream has drained).
  *   prompt_host [B][P], out_token_host [B], out_tokens_host [B][tau] */

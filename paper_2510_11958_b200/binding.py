@@ -6,6 +6,7 @@ runs inside the library's kernels.
 import ctypes as C
 import os
 import re
+from collections import namedtuple
 
 import torch
 
@@ -43,6 +44,12 @@ class _Weights(C.Structure):
 class _State(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_known", "lo_len", "up_len", "cycle", "slot",
                                          "n_emitted", "tau", "L_d")]
+
+
+class _PagedCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("dtype", "n_pages", "page_size", "n_kv_heads", "head_dim")] + \
+               [(n, C.c_int64) for n in ("page_stride", "head_stride", "row_stride")]
 
 
 STATUS = {"OK": 0, "INVALID_ARG": -1, "SHAPE": -2, "STATE": -3, "CAPACITY": -4, "CUDA": -5,
@@ -92,6 +99,10 @@ def load_library():
         "dmtd_get_launch_count": [vp, C.POINTER(i64)],
         "dmtd_debug_set_error_word": [vp, i32],
         "dmtd_attention_decode": [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, C.c_size_t, vp, vp],
+        "dmtd_paged_plan": [vp, vp, i32, i32, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp],
+        "dmtd_paged_append": [vp, vp, vp, i32, i64, i64, i64, i32, i32, vp, vp, C.c_float, C.c_float, vp, vp,
+                              C.POINTER(_PagedCache), vp, vp],
+        "dmtd_paged_attention": [vp, i32, i64, i32, i32, vp, vp, i32, vp, i32, i32, C.POINTER(_PagedCache), vp, C.c_size_t, vp, vp],
         "dmtd_attention_decode_static": [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp],
     }
     for name, args in sig.items():
@@ -336,6 +347,110 @@ def attention_decode_static(q, k, v, pos0, out):
     _, nkv, max_seq, _ = k.shape
     rc = dll.dmtd_attention_decode_static(q.data_ptr(), k.data_ptr(), v.data_ptr(), _KV_CODE[k.dtype], B, R, nq, nkv, D, max_seq, pos0,
                                           out.data_ptr(), _current_stream())
+    if rc:
+        raise DmtdError(rc, dll.dmtd_last_error(None).decode())
+    return out
+
+
+# -- requests of unequal length: a paged KV cache
+
+PAGED_ATTENTION_SCRATCH_BYTES = 48 << 20
+PagedPlan = namedtuple("PagedPlan", "row_start position slot granted lens n_free")
+
+
+def _here(*tensors):
+    """Every tensor is on the current device, whose current stream the call runs on."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or t.get_device() == dev, f"a tensor on {t.device}, the current device is cuda:{dev}"
+
+
+def _ints(*tensors):
+    for t in tensors:
+        assert t.dtype == torch.int32 and t.is_contiguous(), (t.dtype, t.stride())
+
+
+def _paged_cache(k, v):
+    assert k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1 and k.dtype == v.dtype
+    (n_pages, nkv, page, D), (s_page, s_head, s_row, _) = k.shape, k.stride()
+    return C.byref(_PagedCache(k.data_ptr(), v.data_ptr(), _KV_CODE[k.dtype], n_pages, page, nkv, D, s_page, s_head, s_row))
+
+
+def paged_plan(lens, n_new, table, free_pages, n_free, page_size, n_rows, out=None):
+    """Pages and slots for a step's new tokens (dmtd_paged_plan): a PagedPlan of cuda int32 tensors.
+
+    lens, n_new: cuda int32 [B]; table: cuda int32 [B, pages of the longest request], updated in place; free_pages: cuda
+    int32 [pages of the pool], of which the first n_free (cuda int32 [1]) are free, updated in place.  `out`: the
+    six tensors to write to (lens and n_free may be the ones read); without it they are allocated.
+    """
+    dll = _dll or load_library()
+    B, width = table.shape
+    if out is None:
+        out = [torch.empty(n, dtype=torch.int32, device=lens.device) for n in (B + 1, n_rows, n_rows, B, B, 1)]
+    _here(lens, n_new, table, free_pages, n_free, *out)
+    _ints(lens, n_new, table, free_pages, n_free, *out)
+    assert lens.numel() == n_new.numel() == B and n_free.numel() == 1
+    assert tuple(t.numel() for t in out) == (B + 1, n_rows, n_rows, B, B, 1)
+    rc = dll.dmtd_paged_plan(lens.data_ptr(), n_new.data_ptr(), B, page_size, table.data_ptr(), width, free_pages.data_ptr(),
+                             free_pages.numel(), n_free.data_ptr(), n_rows, *(t.data_ptr() for t in out), _current_stream())
+    if rc:
+        raise DmtdError(rc, dll.dmtd_last_error(None).decode())
+    return PagedPlan(*out)
+
+
+def paged_append(q, k, v, position, slot, k_cache, v_cache, q_norm=None, k_norm=None, eps=1e-6, rope_theta=0.0, q_out=None):
+    """QK-norm, rotary embedding and the KV append of new rows (dmtd_paged_append).  Returns q_out [T, nq, D].
+
+    q: cuda [T, nq, D] (or None), k, v: cuda [T, nkv, D], float32, bfloat16 or float16, rows any multiple of 16 bytes
+    apart; position, slot: cuda int32 [T] (PagedPlan); k_cache, v_cache: cuda [pages, nkv, page_size, D] in any order in
+    memory; q_norm, k_norm: cuda float32 [D] or None.  Rows without a slot are left alone, in q_out too.
+    """
+    dll = _dll or load_library()
+    T, nkv, D = k.shape
+    nq = 0 if q is None else q.shape[1]
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _here(q, k, v, position, slot, k_cache, v_cache, q_norm, k_norm, q_out)
+    _ints(position, slot)
+    assert position.numel() == T and slot.numel() == T and v.shape == k.shape and v.dtype == k.dtype
+    assert k_cache.shape[1] == nkv and k_cache.shape[3] == D
+    for t in (q, k, v):
+        assert t is None or (t.shape[0] == T and t.shape[2] == D and t.dtype == k.dtype and t.stride(2) == 1 and t.stride(1) == D)
+    for t in (q_norm, k_norm):
+        assert t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == D)
+    assert q is None or (q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.is_contiguous())
+    rc = dll.dmtd_paged_append(None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), _KV_CODE[k.dtype],
+                               0 if q is None else q.stride(0), k.stride(0), v.stride(0), T, nq,
+                               None if q_norm is None else q_norm.data_ptr(), None if k_norm is None else k_norm.data_ptr(), eps, rope_theta,
+                               position.data_ptr(), slot.data_ptr(), _paged_cache(k_cache, v_cache),
+                               None if q is None else q_out.data_ptr(), _current_stream())
+    if rc:
+        raise DmtdError(rc, dll.dmtd_last_error(None).decode())
+    return q_out
+
+
+def paged_attention(q, row_start, lens, table, k_cache, v_cache, max_new=0, scratch=None, out=None):
+    """Attention of every request's new rows over its pages (dmtd_paged_attention).  Returns out [T, nq, D], type of q.
+
+    q: cuda [T, nq, D], float32 with any cache or of the cache's 16-bit type, rows any multiple of 16 bytes apart; row_start:
+    cuda int32 [B + 1], lens: cuda int32 [B] with the new rows counted, table: cuda int32 [B, pages] (PagedPlan); k_cache,
+    v_cache as in paged_append.  Rows of no request are left as they were in `out` (allocated if not given).
+    `scratch`: a cuda uint8 tensor of PAGED_ATTENTION_SCRATCH_BYTES bytes, allocated through torch if not given.
+    """
+    dll = _dll or load_library()
+    T, nq, D = q.shape
+    B, width = table.shape
+    if scratch is None:
+        scratch = torch.empty(PAGED_ATTENTION_SCRATCH_BYTES, dtype=torch.uint8, device=q.device)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _here(q, row_start, lens, table, k_cache, v_cache, scratch, out)
+    _ints(row_start, lens, table)
+    assert row_start.numel() == B + 1 and lens.numel() == B and k_cache.shape[3] == D and scratch.is_contiguous()
+    assert q.stride(2) == 1 and q.stride(1) == D and out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
+    rc = dll.dmtd_paged_attention(q.data_ptr(), _KV_CODE[q.dtype], q.stride(0), T, nq, row_start.data_ptr(), lens.data_ptr(), B,
+                                  table.data_ptr(), width, max_new, _paged_cache(k_cache, v_cache), scratch.data_ptr(),
+                                  scratch.numel() * scratch.element_size(), out.data_ptr(), _current_stream())
     if rc:
         raise DmtdError(rc, dll.dmtd_last_error(None).decode())
     return out

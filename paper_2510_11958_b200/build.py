@@ -9,10 +9,10 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libdmtd_b200.so")
-SOURCES = ["engine.cu"]
+SOURCES = ["engine.cu", "paged.cu"]
 HEADERS = ["common.cuh", "ptx.cuh", "kernels.cuh", "pass_common.cuh", "pass_stream.cuh", "pass_prologues.cuh",
            "pass_attention.cuh", "pass_attention_f32.cuh", "pass_kernel.cuh", "attention_kernel.cuh", "attention_tc05.cuh",
-           "gemm_tc05.cuh", "small_pass.cuh"]
+           "gemm_tc05.cuh", "small_pass.cuh", "host.h", "paged_common.cuh", "paged_plan.cuh", "paged_append.cuh", "paged_attention.cuh"]
 
 
 def _stale() -> bool:
@@ -30,7 +30,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-           "--use_fast_math" if False else "-DDMTD_NO_FAST_MATH", "-Xcompiler", "-fPIC", "-shared",
+           "--use_fast_math" if False else "-DDMTD_NO_FAST_MATH", "-Xcompiler", "-fPIC", "-shared", "--threads", str(len(SOURCES)),
            "-I", os.path.join(ROOT, "include")]
     cmd += os.environ.get("DMTD_NVCC_FLAGS", "").split()      # e.g. -DDMTD_PASS_SLOTS=2 for an experiment
     if verbose:

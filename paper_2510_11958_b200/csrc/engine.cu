@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "../../include/dmtd.h"
+#include "host.h"
 #include "kernels.cuh"
 #include "pass_kernel.cuh"
 #include "attention_kernel.cuh"
@@ -26,9 +27,10 @@
 
 using namespace dmtd;
 
-namespace {
+// The last error of a call without a context, on this thread.
+static thread_local std::string g_create_error;
 
-thread_local std::string g_create_error;
+namespace {
 
 // Clock ticks a device-side wait (grid barrier, bulk-copy or tensor-core barrier) may spin before
 // it gives up and reports through the context's error word: about a second of SM clock.
@@ -136,6 +138,19 @@ dmtd_status fail(dmtd_ctx *c, dmtd_status st, const char *fmt, ...) {
   if (c) c->err = buf; else g_create_error = buf;
   return st;
 }
+
+}  // namespace
+
+dmtd_status dmtd::call_failed(dmtd_status st, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(nullptr, st, "%s", buf);
+}
+
+namespace {
 
 #define CUDA_TRY(c, expr)                                                                   \
   do {                                                                                      \
@@ -264,34 +279,6 @@ dmtd_status pack_umma(dmtd_ctx *c, UmmaMat *out, int K, const void *const *srcs,
 }
 
 // ---------------------------------------------------------------------------- launches
-
-// Launch with programmatic stream serialisation: the kernel's blocks may become resident while the
-// kernel before it in the stream is still running; it calls griddepcontrol.wait before it touches
-// anything that kernel (or one before it) writes.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
-
-// The same for a grid of clusters of `ranks` blocks.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, int ranks, Args... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = stream;
-  cudaLaunchAttribute attr[2]{};
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = ranks; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr; cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
 
 int gemv_smem_bytes(const PackedMat &W, int NT) {
   int KS = W.aps * 32;

@@ -1,0 +1,180 @@
+// Host side of the paged KV cache's calls (include/dmtd.h): checks of arguments, launches.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "host.h"
+#include "paged_append.cuh"
+#include "paged_attention.cuh"
+#include "paged_plan.cuh"
+
+using namespace dmtd;
+
+namespace {
+
+dmtd_status launched(cudaError_t e, const char *what) {
+  if (e == cudaSuccess) e = cudaGetLastError();
+  return e == cudaSuccess ? DMTD_OK : call_failed(DMTD_ERR_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
+}
+
+size_t dtype_bytes(int t) { return t == DMTD_F32 ? 4 : 2; }
+bool known_dtype(int t) { return t == DMTD_F32 || t == DMTD_BF16 || t == DMTD_F16; }
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// Positions to a page as a power of two; -1: it is none.
+int page_log2(int32_t page_size) {
+  return page_size >= 1 && (page_size & (page_size - 1)) == 0 ? 31 - __builtin_clz((unsigned)page_size) : -1;
+}
+
+dmtd_status pool_check(const char *what, const dmtd_paged_cache *c, PagedPool *out) {
+  if (!c || !c->k || !c->v || c->n_pages < 1) return call_failed(DMTD_ERR_INVALID_ARG, "%s: null cache or no pages", what);
+  if (!known_dtype(c->dtype)) return call_failed(DMTD_ERR_SHAPE, "%s: cache dtype", what);
+  if (c->head_dim != 64 && c->head_dim != 128) return call_failed(DMTD_ERR_SHAPE, "%s: head_dim must be 64 or 128", what);
+  if (c->n_kv_heads < 1) return call_failed(DMTD_ERR_SHAPE, "%s: n_kv_heads", what);
+  const int lg = page_log2(c->page_size);
+  if (lg < 0) return call_failed(DMTD_ERR_SHAPE, "%s: page_size must be a power of two", what);
+  if ((int64_t)c->n_pages << lg > INT32_MAX) return call_failed(DMTD_ERR_CAPACITY, "%s: more than 2^31 - 1 slots", what);
+  *out = PagedPool{c->k, c->v, c->n_pages, lg, c->page_stride, c->head_stride, c->row_stride};
+  if (c->n_pages == 1) out->page_stride = 0;             // (the stride of an axis of one means nothing)
+  if (c->n_kv_heads == 1) out->head_stride = 0;
+  if (c->page_size == 1) out->row_stride = 0;
+  const int64_t unit = 16 / dtype_bytes(c->dtype);
+  const int64_t least = c->head_dim;
+  if ((c->n_pages > 1 && c->page_stride < least) || (c->n_kv_heads > 1 && c->head_stride < least) || (c->page_size > 1 && c->row_stride < least))
+    return call_failed(DMTD_ERR_INVALID_ARG, "%s: a stride of the cache is shorter than a row", what);
+  if (!aligned16(c->k) || !aligned16(c->v) || out->page_stride % unit || out->head_stride % unit || out->row_stride % unit)
+    return call_failed(DMTD_ERR_INVALID_ARG, "%s: the cache's rows must begin on 16-byte boundaries", what);
+  return DMTD_OK;
+}
+
+template <int D, int ROWS>
+cudaError_t append_launch(const PagedAppendParams &P, int act, int kv, dim3 grid, cudaStream_t stream) {
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(APPEND_THREADS), 0, stream, P); };
+  auto by_kv = [&](auto t) {
+    using T = decltype(t);
+    return kv == DMTD_F32 ? go(paged_append_kernel<T, float, D, ROWS>)
+         : kv == DMTD_BF16 ? go(paged_append_kernel<T, __nv_bfloat16, D, ROWS>) : go(paged_append_kernel<T, __half, D, ROWS>);
+  };
+  return act == DMTD_F32 ? by_kv(float{}) : act == DMTD_BF16 ? by_kv(__nv_bfloat16{}) : by_kv(__half{});
+}
+
+template <int D>
+cudaError_t attention_launch(const PagedAttentionParams &P, int qt, int kv, cudaStream_t stream) {
+  const dim3 grid(P.batch.n_rows, (P.nq + 3) / 4);
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(128), 0, stream, P); };
+  if (qt == DMTD_BF16) return go(paged_attention_kernel<__nv_bfloat16, __nv_bfloat16, D>);
+  if (qt == DMTD_F16) return go(paged_attention_kernel<__half, __half, D>);
+  return kv == DMTD_F32 ? go(paged_attention_kernel<float, float, D>)
+       : kv == DMTD_BF16 ? go(paged_attention_kernel<float, __nv_bfloat16, D>) : go(paged_attention_kernel<float, __half, D>);
+}
+
+}  // namespace
+
+extern "C" {
+
+dmtd_status dmtd_paged_plan(const int32_t *lens, const int32_t *n_new, int32_t n_requests, int32_t page_size, int32_t *table,
+                            int32_t table_stride, int32_t *free_pages, int32_t n_pages, const int32_t *n_free, int32_t n_rows,
+                            int32_t *row_start, int32_t *position, int32_t *slot, int32_t *granted, int32_t *lens_out,
+                            int32_t *n_free_out, void *cuda_stream) {
+  if (n_requests < 0 || n_rows < 0 || n_pages < 1 || table_stride < 1)
+    return call_failed(DMTD_ERR_INVALID_ARG, "paged_plan: negative or zero size");
+  if (!free_pages || !n_free || !row_start || !n_free_out || (n_requests && (!lens || !n_new || !table || !granted || !lens_out)) ||
+      (n_rows && (!position || !slot)))
+    return call_failed(DMTD_ERR_INVALID_ARG, "paged_plan: null pointer");
+  const int lg = page_log2(page_size);
+  if (lg < 0) return call_failed(DMTD_ERR_SHAPE, "paged_plan: page_size must be a power of two");
+  if (n_requests > PLAN_MAX_REQUESTS) return call_failed(DMTD_ERR_CAPACITY, "paged_plan: more than %d requests", PLAN_MAX_REQUESTS);
+  if (((int64_t)n_pages << lg) > INT32_MAX || n_pages >= PLAN_MOST || n_rows >= PLAN_MOST || (int64_t)n_requests * table_stride >= PLAN_MOST)
+    return call_failed(DMTD_ERR_CAPACITY, "paged_plan: more than 2^31 - 1 slots, or 2^30 rows or table entries");
+  const PagedPlanParams P{lens, n_new, n_requests, lg, table, table_stride, free_pages, n_pages, n_free, n_rows,
+                          row_start, position, slot, granted, lens_out, n_free_out};
+  const int smem = plan_smem_bytes(n_requests);
+  cudaError_t e = cudaSuccess;
+  if (smem > 48 * 1024) e = cudaFuncSetAttribute(paged_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return call_failed(DMTD_ERR_CUDA, "paged_plan: %s", cudaGetErrorString(e));
+  const int ranks = n_rows > 4 * PLAN_THREADS || n_requests > PLAN_THREADS ? PLAN_CLUSTER : 1;
+  return launched(launch_cluster(paged_plan_kernel, dim3(ranks), dim3(PLAN_THREADS), smem, static_cast<cudaStream_t>(cuda_stream), ranks, P),
+                  "paged_plan");
+}
+
+dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32_t dtype, int64_t q_stride, int64_t k_stride,
+                              int64_t v_stride, int32_t n_rows, int32_t n_q_heads, const float *q_norm, const float *k_norm,
+                              float rms_eps, float rope_theta, const int32_t *position, const int32_t *slot,
+                              const dmtd_paged_cache *cache, void *q_out, void *cuda_stream) {
+  PagedAppendParams P{};
+  const dmtd_status st = pool_check("paged_append", cache, &P.pool);
+  if (st != DMTD_OK) return st;
+  if (n_rows < 0 || n_q_heads < 0) return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: negative size");
+  if (!known_dtype(dtype)) return call_failed(DMTD_ERR_SHAPE, "paged_append: dtype");
+  if (!(rope_theta >= 0.f) || !(rms_eps >= 0.f) || std::isinf(rope_theta)) return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: rope_theta / rms_eps");
+  if (n_rows == 0) return DMTD_OK;
+  if (!k || !v || !position || !slot || (n_q_heads && (!q || !q_out))) return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: null pointer");
+  const int D = cache->head_dim, nkv = cache->n_kv_heads;
+  const int64_t unit = 16 / dtype_bytes(dtype);
+  if (n_rows == 1) q_stride = k_stride = v_stride = 0;
+  else if ((n_q_heads && q_stride < (int64_t)n_q_heads * D) || k_stride < (int64_t)nkv * D || v_stride < (int64_t)nkv * D)
+    return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: a row stride is shorter than a row");
+  if (!aligned16(k) || !aligned16(v) || k_stride % unit || v_stride % unit || (n_q_heads && (!aligned16(q) || !aligned16(q_out) || q_stride % unit)))
+    return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: rows must begin on 16-byte boundaries");
+  P.q = q; P.k = k; P.v = v;
+  P.q_stride = q_stride; P.k_stride = k_stride; P.v_stride = v_stride;
+  P.n_rows = n_rows; P.nq = n_q_heads; P.nkv = nkv;
+  P.q_norm = q_norm; P.k_norm = k_norm; P.eps = rms_eps;
+  P.rotate = rope_theta > 0.f;
+  P.position = position; P.slot = slot; P.q_out = q_out;
+  if (P.rotate) {
+    const double ratio = std::pow((double)rope_theta, -2.0 / D);
+    double f = 0.15915494309189533577;                   // 1 / (2 pi)
+    for (int i = 0; i < D / 2; ++i, f *= ratio) P.turns[i] = f;
+  }
+  const int n_vec = n_q_heads + 2 * nkv;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e;
+  if (n_rows >= 600) {
+    P.per_block = n_vec;
+    const dim3 grid((n_rows + APPEND_ROWS - 1) / APPEND_ROWS, 1);
+    e = D == 128 ? append_launch<128, APPEND_ROWS>(P, dtype, cache->dtype, grid, stream) : append_launch<64, APPEND_ROWS>(P, dtype, cache->dtype, grid, stream);
+  } else {
+    P.per_block = std::min(n_vec, 16);
+    const dim3 grid(n_rows, (n_vec + P.per_block - 1) / P.per_block);
+    e = D == 128 ? append_launch<128, 1>(P, dtype, cache->dtype, grid, stream) : append_launch<64, 1>(P, dtype, cache->dtype, grid, stream);
+  }
+  return launched(e, "paged_append");
+}
+
+dmtd_status dmtd_paged_attention(const void *q, int32_t q_dtype, int64_t q_stride, int32_t n_rows, int32_t n_q_heads,
+                                 const int32_t *row_start, const int32_t *lens, int32_t n_requests, const int32_t *table,
+                                 int32_t table_stride, int32_t max_new, const dmtd_paged_cache *cache, void *scratch,
+                                 size_t scratch_bytes, void *out, void *cuda_stream) {
+  PagedAttentionParams P{};
+  const dmtd_status st = pool_check("paged_attention", cache, &P.pool);
+  if (st != DMTD_OK) return st;
+  const int D = cache->head_dim, nkv = cache->n_kv_heads;
+  if (n_rows < 0 || n_requests < 0 || max_new < 0 || table_stride < 1) return call_failed(DMTD_ERR_INVALID_ARG, "paged_attention: negative or zero size");
+  if (!known_dtype(q_dtype)) return call_failed(DMTD_ERR_SHAPE, "paged_attention: q_dtype");
+  if (q_dtype != DMTD_F32 && q_dtype != cache->dtype)
+    return call_failed(DMTD_ERR_UNSUPPORTED, "paged_attention: 16-bit queries need a cache of their own type");
+  if (n_q_heads < 1 || n_q_heads % nkv || n_q_heads / nkv > 16)
+    return call_failed(DMTD_ERR_SHAPE, "paged_attention: n_q_heads must be a multiple of n_kv_heads, at most 16 per kv head");
+  if ((int64_t)n_rows * n_q_heads > INT32_MAX / 128) return call_failed(DMTD_ERR_CAPACITY, "paged_attention: more than 2^24 query rows and heads");
+  if (n_requests > DMTD_PAGED_MAX_REQUESTS) return call_failed(DMTD_ERR_CAPACITY, "paged_attention: more than %d requests", DMTD_PAGED_MAX_REQUESTS);
+  if (((int64_t)table_stride << P.pool.lg_page) > INT32_MAX)
+    return call_failed(DMTD_ERR_CAPACITY, "paged_attention: a table row names more than 2^31 - 1 positions");
+  if (n_rows == 0 || n_requests == 0) return DMTD_OK;
+  if (!q || !out || !row_start || !lens || !table || !scratch) return call_failed(DMTD_ERR_INVALID_ARG, "paged_attention: null pointer");
+  if (scratch_bytes < DMTD_PAGED_ATTENTION_SCRATCH_BYTES)
+    return call_failed(DMTD_ERR_CAPACITY, "paged_attention: scratch of %zu bytes is smaller than the %zu needed", scratch_bytes,
+                       (size_t)DMTD_PAGED_ATTENTION_SCRATCH_BYTES);
+  if (n_rows == 1) q_stride = 0;
+  else if (q_stride < (int64_t)n_q_heads * D) return call_failed(DMTD_ERR_INVALID_ARG, "paged_attention: the row stride is shorter than a row");
+  if (!aligned16(q) || !aligned16(out) || !aligned16(scratch) || q_stride % (16 / (int64_t)dtype_bytes(q_dtype)))
+    return call_failed(DMTD_ERR_INVALID_ARG, "paged_attention: rows and scratch must begin on 16-byte boundaries");
+  P.q = q; P.q_stride = q_stride; P.out = out;
+  P.batch = PagedBatch{row_start, lens, table, n_requests, table_stride, n_rows};
+  P.nq = n_q_heads; P.nkv = nkv;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  return launched(D == 128 ? attention_launch<128>(P, q_dtype, cache->dtype, stream) : attention_launch<64>(P, q_dtype, cache->dtype, stream),
+                  "paged_attention");
+}
+
+}  // extern "C"

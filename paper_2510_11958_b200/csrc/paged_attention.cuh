@@ -1,0 +1,75 @@
+// Attention of new tokens over a paged cache: dmtd_paged_attention.
+#pragma once
+
+#include "paged_common.cuh"
+
+namespace dmtd {
+
+struct PagedAttentionParams {
+  const void *q;
+  long long q_stride;                        // between rows, in values
+  void *out;                                 // [n_rows][nq][D]
+  PagedBatch batch;
+  PagedPool pool;
+  int nq, nkv;
+};
+
+// One query row and head by one warp, from the definition: scores one by one, softmax with a running maximum.
+template <typename T, typename KVT, int D>
+__device__ __forceinline__ void paged_attend_row(const PagedAttentionParams &P, int b, int row, int seen, int head) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31, kvh = head / (P.nq / P.nkv), lg = P.pool.lg_page;
+  const KVT *kb = reinterpret_cast<const KVT *>(P.pool.k), *vb = reinterpret_cast<const KVT *>(P.pool.v);
+  const int *table = P.batch.table + (size_t)b * P.batch.table_stride;
+  float q[E], o[E], m = -INFINITY, l = 0.f;
+  load_pack(reinterpret_cast<const T *>(P.q) + row * P.q_stride + head * D + lane * E, q);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    q[e] *= rsqrtf((float)D);
+    o[e] = 0.f;
+  }
+  for (int j = 0; j < seen; ++j) {
+    const int page = table[j >> lg];
+    if (page < 0 || page >= P.pool.n_pages) continue;
+    const long long at = P.pool.at(page, kvh, j & ((1 << lg) - 1)) + lane * E;
+    float k[E], v[E], s = 0.f;
+    load_pack(kb + at, k);
+    load_pack(vb + at, v);
+#pragma unroll
+    for (int e = 0; e < E; ++e) s = fmaf(q[e], k[e], s);
+    s = warp_sum(s);
+    if (s == -INFINITY) continue;
+    if (s > m) {
+      const float f = __expf(m - s);
+      m = s;
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= f;
+    }
+    const float p = __expf(s - m);
+    l += p;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(p, v[e], o[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = l != 0.f ? o[e] / l : 0.f;
+  store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o);
+}
+
+// grid (rows, ceil(heads / 4)), a warp to a head
+template <typename T, typename KVT, int D>
+__global__ void __launch_bounds__(128) paged_attention_kernel(const __grid_constant__ PagedAttentionParams P) {
+  paged_enter();
+  const int row = blockIdx.x, head = blockIdx.y * 4 + (threadIdx.x >> 5);
+  if (head >= P.nq) return;
+  // the request whose rows hold this one
+  int lo = 0, hi = P.batch.n_requests;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (P.batch.row(mid + 1) > row) hi = mid; else lo = mid + 1;
+  }
+  if (lo == P.batch.n_requests || row < P.batch.row(lo)) return;
+  paged_attend_row<T, KVT, D>(P, lo, row, P.batch.keys(lo, P.pool.lg_page) - (P.batch.row(lo + 1) - row) + 1, head);
+}
+
+}  // namespace dmtd

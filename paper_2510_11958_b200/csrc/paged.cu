@@ -5,8 +5,8 @@
 
 #include "host.h"
 #include "paged_append.cuh"
-#include "paged_attention.cuh"
 #include "paged_plan.cuh"
+#include "paged_rows.cuh"
 
 using namespace dmtd;
 
@@ -16,6 +16,8 @@ dmtd_status launched(cudaError_t e, const char *what) {
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? DMTD_OK : call_failed(DMTD_ERR_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
 }
+
+constexpr int PAGED_MAX_BLOCKS = 304;                    // blocks of an attention launch, as far as scratch has places
 
 size_t dtype_bytes(int t) { return t == DMTD_F32 ? 4 : 2; }
 bool known_dtype(int t) { return t == DMTD_F32 || t == DMTD_BF16 || t == DMTD_F16; }
@@ -58,14 +60,32 @@ cudaError_t append_launch(const PagedAppendParams &P, int act, int kv, dim3 grid
   return act == DMTD_F32 ? by_kv(float{}) : act == DMTD_BF16 ? by_kv(__nv_bfloat16{}) : by_kv(__half{});
 }
 
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  return n;
+}
+
+template <typename T, typename KVT, int D>
+cudaError_t attention_launch_t(const PagedAttentionParams &P, void *scratch, int n_sms, cudaStream_t stream) {
+  using C = RowsTypes<T, KVT, D>;
+  const int blocks = std::min(2 * n_sms, PAGED_MAX_BLOCKS);
+  const PagedCut K{std::max(1, PR_ROWS / (P.nq / P.nkv)), C::LG_UNIT, 1, INT32_MAX};
+  const PagedScratch S{static_cast<PagedCutItem *>(scratch), reinterpret_cast<float *>(static_cast<PagedCutItem *>(scratch) + PAGED_MAX_BLOCKS), PR_ROWS};
+  static_assert(PAGED_MAX_BLOCKS * (sizeof(PagedCutItem) + 2ull * PR_ROWS * (D + 2) * 4) <= DMTD_PAGED_ATTENTION_SCRATCH_BYTES, "scratch");
+  cudaError_t e = cudaFuncSetAttribute(paged_rows_kernel<T, KVT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e == cudaSuccess) e = launch_pdl(paged_rows_kernel<T, KVT, D>, dim3(blocks), dim3(PR_THREADS), C::SMEM, stream, P, K, S);
+  if (e == cudaSuccess) e = launch_pdl(paged_merge_kernel<T, KVT, D>, dim3(blocks, PR_ROWS / 4), dim3(128), 0, stream, P, S);
+  return e;
+}
+
 template <int D>
-cudaError_t attention_launch(const PagedAttentionParams &P, int qt, int kv, cudaStream_t stream) {
-  const dim3 grid(P.batch.n_rows, (P.nq + 3) / 4);
-  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(128), 0, stream, P); };
-  if (qt == DMTD_BF16) return go(paged_attention_kernel<__nv_bfloat16, __nv_bfloat16, D>);
-  if (qt == DMTD_F16) return go(paged_attention_kernel<__half, __half, D>);
-  return kv == DMTD_F32 ? go(paged_attention_kernel<float, float, D>)
-       : kv == DMTD_BF16 ? go(paged_attention_kernel<float, __nv_bfloat16, D>) : go(paged_attention_kernel<float, __half, D>);
+cudaError_t attention_launch(const PagedAttentionParams &P, int qt, int kv, void *scratch, int n_sms, cudaStream_t stream) {
+  if (qt == DMTD_BF16) return attention_launch_t<__nv_bfloat16, __nv_bfloat16, D>(P, scratch, n_sms, stream);
+  if (qt == DMTD_F16) return attention_launch_t<__half, __half, D>(P, scratch, n_sms, stream);
+  if (kv == DMTD_F32) return attention_launch_t<float, float, D>(P, scratch, n_sms, stream);
+  return kv == DMTD_BF16 ? attention_launch_t<float, __nv_bfloat16, D>(P, scratch, n_sms, stream)
+                         : attention_launch_t<float, __half, D>(P, scratch, n_sms, stream);
 }
 
 }  // namespace
@@ -173,8 +193,10 @@ dmtd_status dmtd_paged_attention(const void *q, int32_t q_dtype, int64_t q_strid
   P.batch = PagedBatch{row_start, lens, table, n_requests, table_stride, n_rows};
   P.nq = n_q_heads; P.nkv = nkv;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  return launched(D == 128 ? attention_launch<128>(P, q_dtype, cache->dtype, stream) : attention_launch<64>(P, q_dtype, cache->dtype, stream),
-                  "paged_attention");
+  const int n_sms = sm_count();
+  if (n_sms < 1) return call_failed(DMTD_ERR_CUDA, "paged_attention: device query failed");
+  return launched(D == 128 ? attention_launch<128>(P, q_dtype, cache->dtype, scratch, n_sms, stream)
+                           : attention_launch<64>(P, q_dtype, cache->dtype, scratch, n_sms, stream), "paged_attention");
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-// Attention of new tokens over a paged cache: dmtd_paged_attention.
+// Attention of new tokens over a paged cache: what its kernels are given, and a row worked out from the definition.
 #pragma once
 
 #include "paged_common.cuh"
@@ -14,9 +14,10 @@ struct PagedAttentionParams {
   int nq, nkv;
 };
 
-// One query row and head by one warp, from the definition: scores one by one, softmax with a running maximum.
+// One query row and head by one warp, from the definition: the keys it sees one by one, softmax with a running maximum.  Slow
+// (a key takes some 100 cycles of latency); for rows that the tiled kernels cannot answer, see there.
 template <typename T, typename KVT, int D>
-__device__ __forceinline__ void paged_attend_row(const PagedAttentionParams &P, int b, int row, int seen, int head) {
+__device__ __noinline__ void paged_attend_row(const PagedAttentionParams &P, int b, int row, int seen, int head) {
   constexpr int E = D / 32;
   const int lane = threadIdx.x & 31, kvh = head / (P.nq / P.nkv), lg = P.pool.lg_page;
   const KVT *kb = reinterpret_cast<const KVT *>(P.pool.k), *vb = reinterpret_cast<const KVT *>(P.pool.v);
@@ -54,22 +55,6 @@ __device__ __forceinline__ void paged_attend_row(const PagedAttentionParams &P, 
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = l != 0.f ? o[e] / l : 0.f;
   store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o);
-}
-
-// grid (rows, ceil(heads / 4)), a warp to a head
-template <typename T, typename KVT, int D>
-__global__ void __launch_bounds__(128) paged_attention_kernel(const __grid_constant__ PagedAttentionParams P) {
-  paged_enter();
-  const int row = blockIdx.x, head = blockIdx.y * 4 + (threadIdx.x >> 5);
-  if (head >= P.nq) return;
-  // the request whose rows hold this one
-  int lo = 0, hi = P.batch.n_requests;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (P.batch.row(mid + 1) > row) hi = mid; else lo = mid + 1;
-  }
-  if (lo == P.batch.n_requests || row < P.batch.row(lo)) return;
-  paged_attend_row<T, KVT, D>(P, lo, row, P.batch.keys(lo, P.pool.lg_page) - (P.batch.row(lo + 1) - row) + 1, head);
 }
 
 }  // namespace dmtd

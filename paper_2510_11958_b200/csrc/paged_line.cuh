@@ -1,0 +1,259 @@
+// The work of a paged attention launch as one line of units, cut into equal shares for its blocks, and the merge of what is cut.
+//
+// An item is a row tile (up to `tile` consecutive new positions of a request, all query heads of one kv head) and the
+// keys that its last position sees, in units of 1 << lg_unit keys.  Items of unequal length follow each other on the
+// line: requests in order, row tiles in order, kv heads.  A block takes an equal share of the line whatever the lengths
+// are, so that there is one wave and no tail.  An item that lies across a border between shares leaves a partial
+// result (unnormalised sums with their level) per block in scratch memory, and paged_merge_kernel joins them; a block has at
+// most two of those, one in front and one behind, so scratch has two places to a block.
+#pragma once
+
+#include "paged_attention.cuh"
+
+namespace dmtd {
+
+// Sum of floor((a i + b) / m) over i = 0 .. n - 1, by exchanging the roles of i and the quotient (a lattice-point
+// count under a line, as in Euclid's algorithm).
+__device__ __forceinline__ long long floor_sum(unsigned long long n, unsigned long long m, unsigned long long a, unsigned long long b) {
+  unsigned long long s = 0;
+  for (;;) {
+    if (a >= m) { s += n * (n - 1) / 2 * (a / m); a %= m; }
+    if (b >= m) { s += n * (b / m); b %= m; }
+    const unsigned long long y = a * n + b;
+    if (y < m) return (long long)s;
+    n = y / m;
+    b = y % m;
+    const unsigned long long t = m; m = a; a = t;
+  }
+}
+
+// Which requests are on a launch's line, and how they are cut.
+struct PagedCut {
+  int tile;                          // positions of a row tile
+  int lg_unit;
+  int min_new, max_new;              // requests of that many new rows
+};
+
+struct PagedRequest {
+  int b, row0, n, c;                 // first row of q, new rows, position of the first of them (may be negative)
+  int tiles;
+  // units of the first m row tiles, for one kv head
+  __device__ __forceinline__ int units(const PagedCut &K, int i) const {
+    const int keys = c + min(n, (i + 1) * K.tile);
+    return keys <= 0 ? 1 : (int)(((unsigned)keys + (1u << K.lg_unit) - 1) >> K.lg_unit);
+  }
+  __device__ __forceinline__ long long units_before(const PagedCut &K, int m) const {
+    if (m == 0) return 0;
+    if (m == 1) return units(K, 0);
+    const int full = min(m, n / K.tile);
+    const int none = c < 0 ? min(full, (int)(-(long long)c / K.tile)) : 0;       // tiles in front of position 0: a unit each
+    long long s = none;
+    if (full > none)
+      s += floor_sum(full - none, 1ull << K.lg_unit, K.tile, (long long)c + (long long)(none + 1) * K.tile + (1 << K.lg_unit) - 1);
+    return m > full ? s + units(K, full) : s;
+  }
+};
+
+__device__ __forceinline__ PagedRequest paged_request(const PagedBatch &batch, int lg_page, const PagedCut &K, int b) {
+  PagedRequest r;
+  r.b = b;
+  r.row0 = batch.row(b);
+  r.n = max(0, batch.row(b + 1) - r.row0);
+  r.c = batch.keys(b, lg_page) - r.n;
+  if (r.n < K.min_new || r.n > K.max_new) r.n = 0;
+  r.tiles = (r.n + K.tile - 1) / K.tile;
+  return r;
+}
+
+// A block's place on the line: an item and the part of its units in the block's share.
+struct PagedPiece {
+  PagedRequest r;
+  int i, kvh;                        // row tile, kv head
+  int t0, t1, per_item;              // units [t0, t1) of per_item
+  __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == per_item; }
+  __device__ __forceinline__ int first(const PagedCut &K) const { return i * K.tile; }
+  __device__ __forceinline__ int rows(const PagedCut &K) const { return min(K.tile, r.n - i * K.tile); }
+  // keys that the tile's last row sees, and position of its first row
+  __device__ __forceinline__ int keys(const PagedCut &K) const { return max(0, r.c + min(r.n, (i + 1) * K.tile)); }
+  __device__ __forceinline__ int position(const PagedCut &K) const { return r.c + i * K.tile; }
+};
+
+// THREADS threads of a block work out the line's length and their block's share.
+template <int THREADS>
+struct PagedShare {
+  long long total, begin, end;
+  int n_blocks;
+  struct Shared {
+    long long upto[THREADS];         // units of the threads' requests up to and with a thread's own
+  };
+
+  // Whole block; `sh` in shared memory.
+  __device__ __forceinline__ void plan(const PagedAttentionParams &P, const PagedCut &K, Shared &sh, int block, int grid) {
+    const int B = P.batch.n_requests, each = (B + THREADS - 1) / THREADS, b0 = threadIdx.x * each;
+    long long mine = 0;
+    if (threadIdx.x < THREADS) {
+      for (int b = b0; b < min(B, b0 + each); ++b) {
+        const PagedRequest r = paged_request(P.batch, P.pool.lg_page, K, b);
+        mine += r.units_before(K, r.tiles) * P.nkv;
+      }
+      // within a warp, then over the warps
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long w = __shfl_up_sync(0xffffffffu, mine, o);
+        if ((threadIdx.x & 31) >= o) mine += w;
+      }
+      sh.upto[threadIdx.x] = mine;
+    }
+    __syncthreads();
+    if (threadIdx.x < THREADS) {
+      for (int w = 0; w < (int)(threadIdx.x >> 5); ++w) mine += sh.upto[w * 32 + 31];
+    }
+    __syncthreads();
+    if (threadIdx.x < THREADS) sh.upto[threadIdx.x] = mine;
+    __syncthreads();
+    total = sh.upto[THREADS - 1];
+    n_blocks = (int)min((long long)grid, total);          // no empty shares: the pieces of an item are consecutive blocks
+    begin = block < n_blocks ? start(block) : total;
+    end = block < n_blocks ? start(block + 1) : total;
+  }
+  __device__ __forceinline__ long long start(int block) const { return total / n_blocks * block + total % n_blocks * block / n_blocks; }
+  // the block that holds unit u
+  __device__ __forceinline__ int holder(long long u) const {
+    int b = (int)min((long long)n_blocks - 1, u / max(1ll, total / n_blocks));
+    while (start(b) > u) --b;
+    while (start(b + 1) <= u) ++b;
+    return b;
+  }
+
+  // The piece that begins at unit u of the line (u < end).
+  __device__ __forceinline__ PagedPiece find(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, long long u) const {
+    int lo = 0, hi = THREADS - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (sh.upto[mid] > u) hi = mid; else lo = mid + 1;
+    }
+    const int B = P.batch.n_requests, each = (B + THREADS - 1) / THREADS;
+    long long v = u - (lo ? sh.upto[lo - 1] : 0);
+    PagedPiece p;
+    for (int b = lo * each;; ++b) {
+      p.r = paged_request(P.batch, P.pool.lg_page, K, b);
+      const long long all = p.r.units_before(K, p.r.tiles) * P.nkv;
+      if (v < all || b + 1 >= B) break;
+      v -= all;
+    }
+    // the row tile: the last whose units begin at or before v
+    int t = 0;
+    for (int top = p.r.tiles; top - t > 1;) {
+      const int mid = (t + top) >> 1;
+      if (p.r.units_before(K, mid) * P.nkv <= v) t = mid; else top = mid;
+    }
+    v -= p.r.units_before(K, t) * P.nkv;
+    p.i = t;
+    p.per_item = p.r.units(K, t);
+    p.kvh = (int)(v / p.per_item);
+    p.t0 = (int)(v - (long long)p.kvh * p.per_item);
+    p.t1 = (int)min((long long)p.per_item, p.t0 + (end - u));
+    return p;
+  }
+  // The piece behind p, which ends at unit u of the line; false: the share ends there.
+  __device__ __forceinline__ bool next(const PagedAttentionParams &P, const PagedCut &K, PagedPiece &p, long long u) const {
+    if (u >= end) return false;
+    if (++p.kvh == P.nkv) {
+      p.kvh = 0;
+      if (++p.i == p.r.tiles) {
+        p.i = 0;
+        int b = p.r.b;
+        do { p.r = paged_request(P.batch, P.pool.lg_page, K, ++b); } while (p.r.n == 0 && b + 1 < P.batch.n_requests);
+      }
+      p.per_item = p.r.units(K, p.i);
+    }
+    p.t0 = 0;
+    p.t1 = (int)min((long long)p.per_item, end - u);
+    return true;
+  }
+};
+
+// What the merge needs to know of an item that begins in a block and goes on behind it.
+struct PagedCutItem {
+  int pieces;                        // 0: the block's last item ends in the block
+  int b, row0, rows, first_seen, kvh;     // request, first row of q, rows, keys that the first row sees
+  int pad[2];
+};
+
+// Scratch: an entry per block, then two partial results per block: [tile rows][D] floats and (level, sum) per row.
+struct PagedScratch {
+  PagedCutItem *items;
+  float *parts;
+  int rows;                          // query rows of a place
+  template <int D> __device__ __forceinline__ float *sums(int place) const { return parts + (size_t)place * rows * (D + 2); }
+  template <int D> __device__ __forceinline__ float2 *levels(int place) const {
+    return reinterpret_cast<float2 *>(sums<D>(place) + (size_t)rows * D);
+  }
+};
+// A block's place for the piece of an item that began in an earlier block / that goes on in a later one.
+__device__ __forceinline__ int paged_place(int block, bool began_here) { return 2 * block + (began_here ? 1 : 0); }
+
+__device__ __forceinline__ PagedCutItem paged_cut_item(const PagedPiece &p, const PagedCut &K, int pieces) {
+  PagedCutItem c{};
+  c.pieces = pieces;
+  c.b = p.r.b;
+  c.row0 = p.r.row0 + p.first(K);
+  c.rows = p.rows(K);
+  c.first_seen = p.position(K) + 1;
+  c.kvh = p.kvh;
+  return c;
+}
+
+// grid (blocks of the attention's launch, row groups), 4 warps: block (j, y) joins rows of the item that is cut at the end of
+// block j's share.  Levels are powers of two.  A warp takes a query row at a time: its lanes fetch the pieces' levels side
+// by side, then all lanes the pieces' sums, which do not depend on each other.
+template <typename T, typename KVT, int D>
+__global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant__ PagedAttentionParams P, PagedScratch S) {
+  constexpr int E = D / 32;
+  paged_enter();
+  const PagedCutItem c = S.items[blockIdx.x];
+  if (c.pieces == 0) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = P.nq / P.nkv;
+  for (int qi = blockIdx.y * 4 + warp; qi < c.rows * G; qi += gridDim.y * 4) {
+    float m = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int s0 = 0; s0 < c.pieces; s0 += 32) {
+      float2 ml = make_float2(-INFINITY, 0.f);
+      auto place = [&](int s) { return paged_place(blockIdx.x + s, s == 0); };
+      if (s0 + lane < c.pieces) ml = __ldcg(&S.levels<D>(place(s0 + lane))[qi]);
+      const float top = fmaxf(m, warp_max(ml.x));
+      const float old = m > -INFINITY ? exp2f(m - top) : 0.f;
+      const float w = ml.x > -INFINITY ? exp2f(ml.x - top) : 0.f;
+      l = l * old + warp_sum(ml.y * w);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= old;
+      const int n = min(32, c.pieces - s0);
+#pragma unroll 8
+      for (int s = 0; s < n; ++s) {
+        const float ws = __shfl_sync(0xffffffffu, w, s);
+        float v[E];
+        load_pack(S.sums<D>(place(s0 + s)) + (size_t)qi * D + lane * E, v);
+        if (ws != 0.f) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] = fmaf(ws, v[e], o[e]);
+        }
+      }
+      m = top;
+    }
+    bool good = true;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      o[e] = l != 0.f ? o[e] / l : 0.f;
+      good = good && isfinite(o[e]);
+    }
+    const int r = qi / G, row = c.row0 + r, head = c.kvh * G + qi % G;
+    if (c.rows > 1 && !__all_sync(0xffffffffu, good)) {
+      paged_attend_row<T, KVT, D>(P, c.b, row, c.first_seen + r, head);
+    } else {
+      store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o);
+    }
+  }
+}
+
+}  // namespace dmtd

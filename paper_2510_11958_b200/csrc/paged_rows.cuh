@@ -1,0 +1,549 @@
+// Attention of a few new rows per request over a paged cache, for every type: split-KV on mma.sync.
+//
+// The G query heads of a kv head for up to 16 / G new positions are the 16 rows of an MMA; every warp streams key tiles of
+// its own (4 KiB of K, 4 KiB of V) through a private ring filled by its own asynchronous copies, no barrier of the
+// block inside the key loop.  The ring runs on across items: the copies' place on the line of work (paged_line.cuh) is
+// two tiles ahead of the arithmetic's, so that HBM is busy under an item's end and the next one's queries.  A tile's page
+// is looked up a tile before its copies are issued.  Pages of fewer positions than a tile has: a lane looks up each
+// key's page, and the lanes that copy a row ask that lane for it.
+//
+// Types.  16-bit queries: one product each for Q K^T and P V, probabilities rounded once to the cache's type, relative to
+// the largest of their own tile (which therefore is not rounded).  fp32 queries: queries and probabilities as two fp16 or three bf16
+// parts, exact to 2^-22 and 2^-24, a product per part; the cache's values are exact as they are.  fp32 cache: everything in two tf32 parts
+// (2^-22), three products.  In those forms a tile's P V is summed from zero and added to the row's sums in fp32.
+//
+// Bound: KV bytes.  An SM's share of HBM is a tile in 360 cycles; its arithmetic takes 260 (32 MMAs) with 16-bit queries.
+#pragma once
+
+#include <type_traits>
+
+#include "paged_line.cuh"
+
+namespace dmtd {
+
+constexpr int PR_WARPS = 4;
+constexpr int PR_THREADS = PR_WARPS * 32;
+constexpr int PR_STAGES = 2;
+constexpr int PR_HALF = 4096;                                  // bytes of a tile's K, and of its V
+constexpr int PR_SLOT = 2 * PR_HALF;
+constexpr int PR_ROWS = 16;                                    // query rows of an item
+constexpr float PR_BELOW = 6.f;                                // a tile's level lies at most this far (in powers of two) below the largest score
+
+// Types of a launch: T queries, KVT cache.
+template <typename T, typename KVT, int D>
+struct RowsTypes {
+  static constexpr bool TF32 = std::is_same<KVT, float>::value;
+  static constexpr int PARTS = TF32 ? 2 : !std::is_same<T, float>::value ? 1 : std::is_same<KVT, __half>::value ? 2 : 3;
+  static constexpr int ROW = D * (int)sizeof(KVT);             // bytes of a key
+  static constexpr int KEYS = PR_HALF / ROW;                   // keys of a tile: 16 (8 to 32)
+  static constexpr int NT = KEYS / 8;
+  static constexpr int COPIES = ROW / 16;                      // 16-byte parts of a row
+  static constexpr int UNIT = PR_WARPS * KEYS;                 // keys of a unit of work
+  static constexpr int LG_UNIT = UNIT == 32 ? 5 : UNIT == 64 ? 6 : 7;
+  // fp16 keeps its full precision down to 2^-14: probabilities are 2^10 times their size there
+  static constexpr float LIFT = std::is_same<KVT, __half>::value ? 10.f : 0.f;
+  static constexpr int QROW = ROW + 16;                        // bytes of a query row in shared memory, free of bank conflicts
+  static constexpr int Q_PARTS = TF32 ? 1 : PARTS;             // tf32: the first part lives in registers
+  static constexpr int OROW = D + 8;
+  static constexpr int Q = PR_WARPS * PR_STAGES * PR_SLOT;
+  static constexpr int OS = Q + Q_PARTS * PR_ROWS * QROW;
+  static constexpr int RED = OS + PR_WARPS * PR_ROWS * OROW * 4;
+  static constexpr int SMEM = RED + 2 * PR_WARPS * PR_ROWS * 4;
+  static_assert(2 * (SMEM + 1024 + 64) <= 228 * 1024, "two blocks per SM");
+  static_assert(sizeof(typename PagedShare<PR_THREADS>::Shared) <= RED - OS, "the line's sums lie where the outputs are put later");
+};
+
+// byte offset of 16-byte part `part` of row `row` in a tile: conflict-free for the copies, for the 16-byte operand loads of K
+// (rows g, parts 4 kb + t) and for ldmatrix on V
+template <int ROW>
+__device__ __forceinline__ uint32_t pr_part(int row, int part) {
+  return (uint32_t)(row * ROW + ((part & ~7) | ((part & 7) ^ (((row & 1) << 2) | ((row >> 1) & 3)))) * 16);
+}
+// ... of an fp32 V tile: lane (g, t) reads part g of rows 2 t and 2 t + 1
+template <int ROW>
+__device__ __forceinline__ uint32_t pr_part_v32(int row, int part) {
+  return (uint32_t)(row * ROW + ((part & ~7) | ((part & 7) ^ (((row >> 1) & 3) << 1))) * 16);
+}
+
+__device__ __forceinline__ uint32_t tf32_of(float x) {
+  uint32_t r;
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void tf32_split(float x, uint32_t &hi, uint32_t &lo) {
+  hi = tf32_of(x);
+  lo = tf32_of(x - __uint_as_float(hi));
+}
+__device__ __forceinline__ void mma_tf32_1688(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// N 16-bit parts of a pair of values, the larger first: x = part 0 + part 1 + ...
+template <class Op, int N>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t (&p)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    p[i] = Op::pack2(x, y);
+    const typename Op::T *h = reinterpret_cast<const typename Op::T *>(&p[i]);
+    x -= Op::to_float(h[0]);
+    y -= Op::to_float(h[1]);
+  }
+}
+
+// Running sums of 16 query rows: lane (g, t) holds rows g and g + 8.  16-bit: n-tile j holds dimensions 8 j + 2 t, + 1;
+// tf32: n-tile 4 blk + j holds dimensions 32 blk + 8 t + j, + 4.
+template <int D>
+struct RowsAcc {
+  float m[2], l[2], top[2];          // per row: level of the sums (powers of two), this lane's share of the sum, largest score
+  float o[D / 8][4];
+  __device__ __forceinline__ void clear() {
+    m[0] = m[1] = top[0] = top[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  }
+};
+
+// A warp's tile of keys against the 16 query rows.  q_t: the queries in shared memory; qh: what of them is in registers.
+// lim[h]: keys that row g + 8 h sees, counted from the tile's first; good: a bit per key that is there at all.
+template <class C, typename KVT, int D, class QRegs>
+__device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t v_t, uint32_t q_t, const QRegs &qh, float scale,
+                                          const int (&lim)[2], uint32_t good, bool mask) {
+  using Op = typename std::conditional<std::is_same<KVT, __half>::value, OpF16, OpBf16>::type;
+  constexpr int NT = C::NT;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  float c[NT][4];
+  if constexpr (C::TF32) {
+    float lo[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
+      lo[j][0] = lo[j][1] = lo[j][2] = lo[j][3] = 0.f;
+    }
+#pragma unroll
+    for (int kb = 0; kb < D / 16; ++kb) {
+      const uint4 l0 = lds128(q_t + g * C::QROW + kb * 64 + t * 16), l1 = lds128(q_t + (g + 8) * C::QROW + kb * 64 + t * 16);
+      const uint4 h0 = qh.v[kb][0], h1 = qh.v[kb][1];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const uint4 k = lds128(k_t + pr_part<C::ROW>(j * 8 + g, kb * 4 + t));
+        uint32_t kh[4], kl[4];
+        tf32_split(__uint_as_float(k.x), kh[0], kl[0]);
+        tf32_split(__uint_as_float(k.y), kh[1], kl[1]);
+        tf32_split(__uint_as_float(k.z), kh[2], kl[2]);
+        tf32_split(__uint_as_float(k.w), kh[3], kl[3]);
+        mma_tf32_1688(c[j], h0.x, h1.x, h0.y, h1.y, kh[0], kh[1]);
+        mma_tf32_1688(lo[j], h0.x, h1.x, h0.y, h1.y, kl[0], kl[1]);
+        mma_tf32_1688(lo[j], l0.x, l1.x, l0.y, l1.y, kh[0], kh[1]);
+        mma_tf32_1688(c[j], h0.z, h1.z, h0.w, h1.w, kh[2], kh[3]);
+        mma_tf32_1688(lo[j], h0.z, h1.z, h0.w, h1.w, kl[2], kl[3]);
+        mma_tf32_1688(lo[j], l0.z, l1.z, l0.w, l1.w, kh[2], kh[3]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[j][e] = (c[j][e] + lo[j][e]) * scale;
+    }
+  } else {
+    float c2[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
+      c2[j][0] = c2[j][1] = c2[j][2] = c2[j][3] = 0.f;
+    }
+#pragma unroll
+    for (int kb = 0; kb < D / 32; ++kb) {
+      uint4 k[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) k[j] = lds128(k_t + pr_part<C::ROW>(j * 8 + g, kb * 4 + t));
+#pragma unroll
+      for (int part = 0; part < C::PARTS; ++part) {
+        uint4 h0, h1;
+        if constexpr (C::PARTS == 1) {
+          h0 = qh.v[kb][0];
+          h1 = qh.v[kb][1];
+        } else {
+          const uint32_t at = q_t + part * PR_ROWS * C::QROW + g * C::QROW + kb * 64 + t * 16;
+          h0 = lds128(at);
+          h1 = lds128(at + 8 * C::QROW);
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          // the larger parts' products in sums of their own
+          Op::mma(part ? c2[j] : c[j], h0.x, h1.x, h0.y, h1.y, k[j].x, k[j].y);
+          Op::mma(part || C::PARTS == 1 ? c2[j] : c[j], h0.z, h1.z, h0.w, h1.w, k[j].z, k[j].w);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[j][e] = (c[j][e] + c2[j][e]) * scale;
+    }
+  }
+  if (mask) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = j * 8 + 2 * t + (e & 1);
+        if (key >= lim[e >> 1] || !((good >> key) & 1)) c[j][e] = -INFINITY;
+      }
+    }
+  }
+  float corr[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float mx = fmaxf(c[0][2 * h], c[0][2 * h + 1]);
+#pragma unroll
+    for (int j = 1; j < NT; ++j) mx = fmaxf(mx, fmaxf(c[j][2 * h], c[j][2 * h + 1]));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+    A.top[h] = fmaxf(A.top[h], mx);
+    const float level = fmaxf(mx, A.top[h] - PR_BELOW) - C::LIFT;
+    corr[h] = level > -INFINITY ? exp2_approx(A.m[h] - level) : 1.f;
+    A.m[h] = level;
+  }
+  float sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      c[j][e] = c[j][e] == -INFINITY ? 0.f : exp2_approx(c[j][e] - A.m[e >> 1]);       // (NaN stays)
+      sum[e >> 1] += c[j][e];
+    }
+  }
+  A.l[0] = A.l[0] * corr[0] + sum[0];
+  A.l[1] = A.l[1] * corr[1] + sum[1];
+  if constexpr (C::TF32) {
+    // column k = t of the A operand is key 2 t, column t + 4 key 2 t + 1
+    uint32_t ph[NT][4], pl[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      tf32_split(c[j][0], ph[j][0], pl[j][0]);
+      tf32_split(c[j][2], ph[j][1], pl[j][1]);
+      tf32_split(c[j][1], ph[j][2], pl[j][2]);
+      tf32_split(c[j][3], ph[j][3], pl[j][3]);
+    }
+#pragma unroll
+    for (int blk = 0; blk < D / 32; ++blk) {
+      float s[4][4], lo[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+        lo[i][0] = lo[i][1] = lo[i][2] = lo[i][3] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const uint4 v0 = lds128(v_t + pr_part_v32<C::ROW>(j * 8 + 2 * t, blk * 8 + g));
+        const uint4 v1 = lds128(v_t + pr_part_v32<C::ROW>(j * 8 + 2 * t + 1, blk * 8 + g));
+        const uint32_t a[4] = {v0.x, v0.y, v0.z, v0.w}, b[4] = {v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t ah, al, bh, bl;
+          tf32_split(__uint_as_float(a[i]), ah, al);
+          tf32_split(__uint_as_float(b[i]), bh, bl);
+          mma_tf32_1688(s[i], ph[j][0], ph[j][1], ph[j][2], ph[j][3], ah, bh);
+          mma_tf32_1688(lo[i], ph[j][0], ph[j][1], ph[j][2], ph[j][3], al, bl);
+          mma_tf32_1688(lo[i], pl[j][0], pl[j][1], pl[j][2], pl[j][3], ah, bh);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) A.o[blk * 4 + i][e] = fmaf(A.o[blk * 4 + i][e], corr[e >> 1], s[i][e] + lo[i][e]);
+      }
+    }
+  } else {
+    constexpr int KS = NT / 2;
+    uint32_t p[KS][4][C::PARTS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) split_pair<Op, C::PARTS>(c[2 * ks + (i >> 1)][(i & 1) * 2], c[2 * ks + (i >> 1)][(i & 1) * 2 + 1], p[ks][i]);
+    }
+    const int mi = lane >> 3, rr = (mi & 1) * 8 + (lane & 7);
+#pragma unroll
+    for (int d2 = 0; d2 < D / 16; ++d2) {
+      if constexpr (C::PARTS == 1) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float(&o)[4] = A.o[2 * d2 + h];
+          o[0] *= corr[0]; o[1] *= corr[0]; o[2] *= corr[1]; o[3] *= corr[1];
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          uint32_t b0, b1, b2, b3;
+          ldmatrix_x4_trans(v_t + pr_part<C::ROW>(ks * 16 + rr, d2 * 2 + (mi >> 1)), b0, b1, b2, b3);
+          Op::mma(A.o[2 * d2], p[ks][0][0], p[ks][1][0], p[ks][2][0], p[ks][3][0], b0, b1);
+          Op::mma(A.o[2 * d2 + 1], p[ks][0][0], p[ks][1][0], p[ks][2][0], p[ks][3][0], b2, b3);
+        }
+      } else {
+        float s[2][4], lo[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          s[h][0] = s[h][1] = s[h][2] = s[h][3] = 0.f;
+          lo[h][0] = lo[h][1] = lo[h][2] = lo[h][3] = 0.f;
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          uint32_t b0, b1, b2, b3;
+          ldmatrix_x4_trans(v_t + pr_part<C::ROW>(ks * 16 + rr, d2 * 2 + (mi >> 1)), b0, b1, b2, b3);
+#pragma unroll
+          for (int part = 0; part < C::PARTS; ++part) {
+            Op::mma(part ? lo[0] : s[0], p[ks][0][part], p[ks][1][part], p[ks][2][part], p[ks][3][part], b0, b1);
+            Op::mma(part ? lo[1] : s[1], p[ks][0][part], p[ks][1][part], p[ks][2][part], p[ks][3][part], b2, b3);
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) A.o[2 * d2 + h][e] = fmaf(A.o[2 * d2 + h][e], corr[e >> 1], s[h][e] + lo[h][e]);
+        }
+      }
+    }
+  }
+}
+
+template <typename C, int D>
+struct RowsQueries {                 // what of the queries is in registers: all (one part), or the first of two tf32 parts
+  uint4 v[C::TF32 ? D / 16 : D / 32][2];
+};
+
+template <typename T, typename KVT, int D>
+__global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_constant__ PagedAttentionParams P, PagedCut K, PagedScratch S) {
+  using C = RowsTypes<T, KVT, D>;
+  using Op = typename std::conditional<std::is_same<KVT, __half>::value, OpF16, OpBf16>::type;
+  extern __shared__ __align__(128) unsigned char sc[];
+  auto &line = *reinterpret_cast<typename PagedShare<PR_THREADS>::Shared *>(sc + C::OS);
+  __shared__ uint32_t there[PR_WARPS][PR_STAGES];              // a bit per key of a ring slot
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int G = P.nq / P.nkv, lg = P.pool.lg_page;
+  paged_enter();
+  PagedShare<PR_THREADS> share;
+  share.plan(P, K, line, blockIdx.x, gridDim.x);
+  if (share.begin >= share.end) {
+    if (threadIdx.x == 0) S.items[blockIdx.x].pieces = 0;
+    return;
+  }
+  const uint32_t ring = smem_u32(sc) + warp * PR_STAGES * PR_SLOT, q_t = smem_u32(sc) + C::Q;
+  float *const o_s = reinterpret_cast<float *>(sc + C::OS), *const red_m = reinterpret_cast<float *>(sc + C::RED);
+  float *const red_l = red_m + PR_WARPS * PR_ROWS;
+  const float scale = 1.4426950408889634f * rsqrtf((float)D);
+  const KVT *const kb = reinterpret_cast<const KVT *>(P.pool.k), *const vb = reinterpret_cast<const KVT *>(P.pool.v);
+
+  // ---- the copies' place on the line: the piece, its next unit, the page of the lane's key of that unit's tile
+  PagedPiece ahead = share.find(P, K, line, share.begin);
+  long long ahead_end = share.begin + (ahead.t1 - ahead.t0);   // of the piece, on the line
+  int ahead_unit = ahead.t0, ahead_keys = ahead.keys(K), page_id = -1;
+  bool ahead_on = true;
+  const int copy_part = lane % C::COPIES, copy_row = lane / C::COPIES;
+  constexpr int COPY_ROWS = 32 / C::COPIES;                    // rows of one instruction
+  auto look_up = [&]() {
+    const int key = ahead_unit * C::UNIT + warp * C::KEYS + (lane & (C::KEYS - 1));
+    page_id = key < ahead_keys ? P.batch.table[(size_t)ahead.r.b * P.batch.table_stride + (key >> lg)] : -1;
+  };
+  look_up();
+  auto fetch = [&](int slot) {
+    if (ahead_on) {
+      const int key0 = ahead_unit * C::UNIT + warp * C::KEYS;
+      const bool ok = page_id >= 0 && page_id < P.pool.n_pages;                 // (keys beyond the last have no page)
+      const uint32_t mask = __ballot_sync(0xffffffffu, ok);
+      if (lane == 0) there[warp][slot] = C::KEYS == 32 ? mask : mask & ((1u << C::KEYS) - 1);
+      const uint32_t dst = ring + slot * PR_SLOT;
+      if (lg >= (C::KEYS == 8 ? 3 : C::KEYS == 16 ? 4 : 5)) {
+        // the tile lies in one page
+        const int id = __shfl_sync(0xffffffffu, page_id, 0);
+        const long long at = id >= 0 && id < P.pool.n_pages
+                                 ? P.pool.at(id, ahead.kvh, (key0 & ((1 << lg) - 1)) + copy_row) + copy_part * (16 / (int)sizeof(KVT)) : 0;
+#pragma unroll
+        for (int j = 0; j < C::KEYS / COPY_ROWS; ++j) {
+          const int row = j * COPY_ROWS + copy_row, bytes = (mask >> row) & 1 ? 16 : 0;
+          const long long src = bytes ? at + j * COPY_ROWS * P.pool.row_stride : 0;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pr_part<C::ROW>(row, copy_part)), "l"(kb + src), "r"(bytes) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                           dst + PR_HALF + (C::TF32 ? pr_part_v32<C::ROW>(row, copy_part) : pr_part<C::ROW>(row, copy_part))),
+                       "l"(vb + src), "r"(bytes) : "memory");
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < C::KEYS / COPY_ROWS; ++j) {
+          const int row = j * COPY_ROWS + copy_row, bytes = (mask >> row) & 1 ? 16 : 0;
+          const int id = __shfl_sync(0xffffffffu, page_id, row);
+          const long long src = bytes ? P.pool.at(id, ahead.kvh, (key0 + row) & ((1 << lg) - 1)) + copy_part * (16 / (int)sizeof(KVT)) : 0;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pr_part<C::ROW>(row, copy_part)), "l"(kb + src), "r"(bytes) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                           dst + PR_HALF + (C::TF32 ? pr_part_v32<C::ROW>(row, copy_part) : pr_part<C::ROW>(row, copy_part))),
+                       "l"(vb + src), "r"(bytes) : "memory");
+        }
+      }
+      if (++ahead_unit == ahead.t1) {
+        ahead_on = share.next(P, K, ahead, ahead_end);
+        ahead_end += ahead.t1 - ahead.t0;
+        ahead_unit = ahead.t0;
+        ahead_keys = ahead.keys(K);
+      }
+      if (ahead_on) look_up();
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");       // an empty group past the share keeps the counts uniform
+  };
+
+  PagedPiece piece = ahead;
+  long long piece_end = ahead_end;
+  int slot = 0;
+#pragma unroll
+  for (int s = 0; s < PR_STAGES; ++s) fetch(s);
+
+  for (;;) {
+    const int rows = piece.rows(K), nQ = rows * G, n_keys = piece.keys(K), pos = piece.position(K);
+    const int row0 = piece.r.row0 + piece.first(K);
+    // ---- queries: row qi = (row row0 + qi / G, head kvh * G + qi % G); beyond nQ zero
+    for (int idx = threadIdx.x; idx < PR_ROWS * (D / 8); idx += PR_THREADS) {
+      const int qi = idx / (D / 8), d = idx % (D / 8) * 8;
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = 0.f;
+      if (qi < nQ) load_pack(reinterpret_cast<const T *>(P.q) + (row0 + qi / G) * P.q_stride + (piece.kvh * G + qi % G) * D + d, f);
+      if constexpr (C::TF32) {
+        float *dst = reinterpret_cast<float *>(sc + C::Q + qi * C::QROW) + d;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dst[j] = f[j];
+      } else {
+        uint32_t w[4][C::PARTS];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) split_pair<Op, C::PARTS>(f[2 * j], f[2 * j + 1], w[j]);
+#pragma unroll
+        for (int part = 0; part < C::PARTS; ++part)
+          sts128(q_t + (part * PR_ROWS + qi) * C::QROW + d * 2, make_uint4(w[0][part], w[1][part], w[2][part], w[3][part]));
+      }
+    }
+    __syncthreads();
+    RowsQueries<C, D> qh;
+    if constexpr (C::TF32) {
+      // the first parts to registers; what remains takes their place
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint4 x = lds128(q_t + (g + 8 * h) * C::QROW + k * 64 + t * 16);
+          qh.v[k][h] = make_uint4(tf32_of(__uint_as_float(x.x)), tf32_of(__uint_as_float(x.y)), tf32_of(__uint_as_float(x.z)), tf32_of(__uint_as_float(x.w)));
+        }
+      }
+      __syncthreads();
+      if (warp == 0) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t at = q_t + (g + 8 * h) * C::QROW + k * 64 + t * 16;
+            const uint4 x = lds128(at), y = qh.v[k][h];
+            sts128(at, make_uint4(tf32_of(__uint_as_float(x.x) - __uint_as_float(y.x)), tf32_of(__uint_as_float(x.y) - __uint_as_float(y.y)),
+                                  tf32_of(__uint_as_float(x.z) - __uint_as_float(y.z)), tf32_of(__uint_as_float(x.w) - __uint_as_float(y.w))));
+          }
+        }
+      }
+      __syncthreads();
+    } else if constexpr (C::PARTS == 1) {
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        qh.v[k][0] = lds128(q_t + g * C::QROW + k * 64 + t * 16);
+        qh.v[k][1] = lds128(q_t + (g + 8) * C::QROW + k * 64 + t * 16);
+      }
+    }
+
+    // ---- keys
+    RowsAcc<D> A;
+    A.clear();
+    const int lim0[2] = {min(n_keys, pos + g / G + 1), min(n_keys, pos + (g + 8) / G + 1)};
+    for (int i = piece.t0; i < piece.t1; ++i) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(PR_STAGES - 1) : "memory");
+      __syncwarp();
+      const int key0 = i * C::UNIT + warp * C::KEYS;
+      const uint32_t k_t = ring + slot * PR_SLOT;
+      if (key0 < n_keys) {
+        const uint32_t good = there[warp][slot];
+        const int lim[2] = {lim0[0] - key0, lim0[1] - key0};
+        rows_tile<C, KVT, D>(A, k_t, k_t + PR_HALF, q_t, qh, scale, lim, good,
+                             key0 + C::KEYS > pos + 1 || good != (C::KEYS == 32 ? 0xffffffffu : (1u << C::KEYS) - 1));
+      }
+      __syncwarp();                                            // the slot is free
+      fetch(slot);
+      if (++slot == PR_STAGES) slot = 0;
+    }
+
+    // ---- the warps' results to shared memory, joined there
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float l = A.l[h];
+      l += __shfl_xor_sync(0xffffffffu, l, 1);
+      l += __shfl_xor_sync(0xffffffffu, l, 2);
+      const int q = g + 8 * h;
+      if (t == 0) { red_m[warp * PR_ROWS + q] = A.m[h]; red_l[warp * PR_ROWS + q] = l; }
+      if (q < nQ) {
+        float *row = o_s + (warp * PR_ROWS + q) * C::OROW;
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j) {
+          if constexpr (C::TF32) {
+            row[(j >> 2) * 32 + 8 * t + (j & 3)] = A.o[j][2 * h];
+            row[(j >> 2) * 32 + 8 * t + (j & 3) + 4] = A.o[j][2 * h + 1];
+          } else {
+            *reinterpret_cast<float2 *>(row + j * 8 + 2 * t) = make_float2(A.o[j][2 * h], A.o[j][2 * h + 1]);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    const bool whole = piece.whole();
+    const int place = paged_place(blockIdx.x, piece.t0 == 0);
+    bool good = true;
+    for (int idx = threadIdx.x; idx < nQ * (D / 4); idx += PR_THREADS) {
+      const int qi = idx / (D / 4), d = idx % (D / 4) * 4;
+      float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < PR_WARPS; ++w) m = fmaxf(m, red_m[w * PR_ROWS + qi]);
+#pragma unroll
+      for (int w = 0; w < PR_WARPS; ++w) {
+        const float mw = red_m[w * PR_ROWS + qi];
+        if (mw > -INFINITY) {                                  // (a warp without keys has none)
+          const float f = exp2_approx(mw - m);
+          const float4 v = *reinterpret_cast<const float4 *>(o_s + (w * PR_ROWS + qi) * C::OROW + d);
+          l = fmaf(red_l[w * PR_ROWS + qi], f, l);
+          acc[0] = fmaf(v.x, f, acc[0]); acc[1] = fmaf(v.y, f, acc[1]); acc[2] = fmaf(v.z, f, acc[2]); acc[3] = fmaf(v.w, f, acc[3]);
+        }
+      }
+      if (whole) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          acc[j] = l != 0.f ? acc[j] / l : 0.f;
+          good = good && isfinite(acc[j]);
+        }
+        store_pack(reinterpret_cast<T *>(P.out) + ((size_t)(row0 + qi / G) * P.nq + piece.kvh * G + qi % G) * D + d, acc);
+      } else {
+        store_pack(S.sums<D>(place) + (size_t)qi * D + d, acc);
+        if (d == 0) S.levels<D>(place)[qi] = make_float2(m, l);
+      }
+    }
+    // A row that is not finite: a probability of zero may have met an infinity or a NaN in a row of V that it does not see
+    // (a later one of the same tile).  Such tiles are worked out again row by row.
+    if (__syncthreads_or(rows > 1 && !good)) {
+      for (int qi = warp; qi < nQ; qi += PR_WARPS)
+        paged_attend_row<T, KVT, D>(P, piece.r.b, row0 + qi / G, pos + qi / G + 1, piece.kvh * G + qi % G);
+    }
+    const bool cut_behind = piece.t0 == 0 && !whole;
+    if (piece_end >= share.end) {
+      if (threadIdx.x == 0) {
+        // the item goes on for per_item - t1 units behind the share
+        const int pieces = cut_behind ? share.holder(piece_end - 1 + (piece.per_item - piece.t1)) - (int)blockIdx.x + 1 : 0;
+        S.items[blockIdx.x] = paged_cut_item(piece, K, pieces);
+      }
+      break;
+    }
+    share.next(P, K, piece, piece_end);
+    piece_end += piece.t1 - piece.t0;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+}  // namespace dmtd

@@ -1,7 +1,8 @@
 // The work of a paged attention launch as one line of units, cut into equal shares for its blocks, and the merge of what is cut.
 //
 // An item is a row tile (up to `tile` consecutive new positions of a request, all query heads of one kv head) and the
-// keys that its last position sees, in units of 1 << lg_unit keys.  Items of unequal length follow each other on the
+// keys that its last position sees, in units of 1 << lg_unit keys; one unit in front of them stands for what an item costs
+// whatever its length is (queries, joining the warps, storing).  Items of unequal length follow each other on the
 // line: requests in order, row tiles in order, kv heads.  A block takes an equal share of the line whatever the lengths
 // are, so that there is one wave and no tail.  An item that lies across a border between shares leaves a partial
 // result (unnormalised sums with their level) per block in scratch memory, and paged_merge_kernel joins them; a block has at
@@ -37,17 +38,17 @@ struct PagedCut {
 struct PagedRequest {
   int b, row0, n, c;                 // first row of q, new rows, position of the first of them (may be negative)
   int tiles;
-  // units of the first m row tiles, for one kv head
+  // units of row tile i, and of the first m row tiles, for one kv head
   __device__ __forceinline__ int units(const PagedCut &K, int i) const {
     const int keys = c + min(n, (i + 1) * K.tile);
-    return keys <= 0 ? 1 : (int)(((unsigned)keys + (1u << K.lg_unit) - 1) >> K.lg_unit);
+    return 1 + (keys <= 0 ? 0 : (int)(((unsigned)keys + (1u << K.lg_unit) - 1) >> K.lg_unit));
   }
   __device__ __forceinline__ long long units_before(const PagedCut &K, int m) const {
     if (m == 0) return 0;
     if (m == 1) return units(K, 0);
     const int full = min(m, n / K.tile);
-    const int none = c < 0 ? min(full, (int)(-(long long)c / K.tile)) : 0;       // tiles in front of position 0: a unit each
-    long long s = none;
+    const int none = c < 0 ? min(full, (int)(-(long long)c / K.tile)) : 0;       // tiles in front of position 0
+    long long s = full;
     if (full > none)
       s += floor_sum(full - none, 1ull << K.lg_unit, K.tile, (long long)c + (long long)(none + 1) * K.tile + (1 << K.lg_unit) - 1);
     return m > full ? s + units(K, full) : s;
@@ -69,10 +70,13 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedBatch &batch, i
 struct PagedPiece {
   PagedRequest r;
   int i, kvh;                        // row tile, kv head
-  int t0, t1, per_item;              // units [t0, t1) of per_item
+  int t0, t1, per_item;              // units [t0, t1) of per_item, the one in front among them
   __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == per_item; }
   __device__ __forceinline__ int first(const PagedCut &K) const { return i * K.tile; }
   __device__ __forceinline__ int rows(const PagedCut &K) const { return min(K.tile, r.n - i * K.tile); }
+  // the piece's units of keys
+  __device__ __forceinline__ int key_begin() const { return max(t0 - 1, 0); }
+  __device__ __forceinline__ int key_end() const { return t1 - 1; }
   // keys that the tile's last row sees, and position of its first row
   __device__ __forceinline__ int keys(const PagedCut &K) const { return max(0, r.c + min(r.n, (i + 1) * K.tile)); }
   __device__ __forceinline__ int position(const PagedCut &K) const { return r.c + i * K.tile; }

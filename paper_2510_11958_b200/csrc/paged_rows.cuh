@@ -3,9 +3,9 @@
 // The G query heads of a kv head for up to 16 / G new positions are the 16 rows of an MMA; every warp streams key tiles of
 // its own (4 KiB of K, 4 KiB of V) through a private ring filled by its own asynchronous copies, no barrier of the
 // block inside the key loop.  The ring runs on across items: the copies' place on the line of work (paged_line.cuh) is
-// two tiles ahead of the arithmetic's, so that HBM is busy under an item's end and the next one's queries.  A tile's page
-// is looked up a tile before its copies are issued.  Pages of fewer positions than a tile has: a lane looks up each
-// key's page, and the lanes that copy a row ask that lane for it.
+// two tiles ahead of the arithmetic's, so that HBM is busy under an item's end and the next one's queries.  Page ids are read
+// 32 at a time, long before they are needed.  Pages of fewer positions than a tile has: a lane looks up each
+// key's page a tile ahead, and the lanes that copy a row ask that lane for it.
 //
 // Types.  16-bit queries: one product each for Q K^T and P V, probabilities rounded once to the cache's type, relative to
 // the largest of their own tile (which therefore is not rounded).  fp32 queries: queries and probabilities as two fp16 or three bf16
@@ -334,58 +334,87 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
   const float scale = 1.4426950408889634f * rsqrtf((float)D);
   const KVT *const kb = reinterpret_cast<const KVT *>(P.pool.k), *const vb = reinterpret_cast<const KVT *>(P.pool.v);
 
-  // ---- the copies' place on the line: the piece, its next unit, the page of the lane's key of that unit's tile
+  // ---- the copies' place on the line: the piece, its next unit of keys, the page ids at hand
   PagedPiece ahead = share.find(P, K, line, share.begin);
   long long ahead_end = share.begin + (ahead.t1 - ahead.t0);   // of the piece, on the line
-  int ahead_unit = ahead.t0, ahead_keys = ahead.keys(K), page_id = -1;
+  int ahead_unit = ahead.key_begin(), ahead_keys = ahead.keys(K);
   bool ahead_on = true;
   const int copy_part = lane % C::COPIES, copy_row = lane / C::COPIES;
   constexpr int COPY_ROWS = 32 / C::COPIES;                    // rows of one instruction
-  auto look_up = [&]() {
-    const int key = ahead_unit * C::UNIT + warp * C::KEYS + (lane & (C::KEYS - 1));
-    page_id = key < ahead_keys ? P.batch.table[(size_t)ahead.r.b * P.batch.table_stride + (key >> lg)] : -1;
+  constexpr int LG_KEYS = C::KEYS == 8 ? 3 : C::KEYS == 16 ? 4 : 5;
+  const bool one_page = lg >= LG_KEYS;                         // a tile lies in one page
+  // one_page: lane i has the id of page page0 + i, and once they are asked for of page page0 + 32 + i; else lane i has that
+  // of the page of the next tile's key i
+  int ids = -1, ids_next = -1, page0 = 0;
+  bool asked = false;
+  auto page_at = [&](int page) {
+    return ((long long)page << lg) < ahead_keys ? P.batch.table[(size_t)ahead.r.b * P.batch.table_stride + page] : -1;
   };
-  look_up();
+  auto tile_key = [&]() { return ahead_unit * C::UNIT + warp * C::KEYS; };
+  auto look_up = [&](bool new_piece) {
+    if (!one_page) {
+      ids = page_at((tile_key() + (lane & (C::KEYS - 1))) >> lg);
+      return;
+    }
+    const int page = tile_key() >> lg;
+    if (new_piece) {
+      page0 = page;
+      ids = page_at(page0 + lane);
+      asked = false;
+    } else if (page - page0 >= 32) {                           // (a unit spans four pages at most)
+      page0 += 32;
+      ids = ids_next;
+      asked = false;
+    } else if (page - page0 >= 16 && !asked) {
+      ids_next = page_at(page0 + 32 + lane);
+      asked = true;
+    }
+  };
+  auto skip_empty = [&]() {                                    // pieces without keys have no copies
+    while (ahead_on && ahead_unit >= ahead.key_end()) {
+      ahead_on = share.next(P, K, ahead, ahead_end);
+      ahead_end += ahead.t1 - ahead.t0;
+      ahead_unit = ahead.key_begin();
+      ahead_keys = ahead.keys(K);
+    }
+  };
   auto fetch = [&](int slot) {
     if (ahead_on) {
-      const int key0 = ahead_unit * C::UNIT + warp * C::KEYS;
-      const bool ok = page_id >= 0 && page_id < P.pool.n_pages;                 // (keys beyond the last have no page)
-      const uint32_t mask = __ballot_sync(0xffffffffu, ok);
-      if (lane == 0) there[warp][slot] = C::KEYS == 32 ? mask : mask & ((1u << C::KEYS) - 1);
+      const int key0 = tile_key(), left = ahead_keys - key0;  // keys from the tile's first on
       const uint32_t dst = ring + slot * PR_SLOT;
-      if (lg >= (C::KEYS == 8 ? 3 : C::KEYS == 16 ? 4 : 5)) {
-        // the tile lies in one page
-        const int id = __shfl_sync(0xffffffffu, page_id, 0);
-        const long long at = id >= 0 && id < P.pool.n_pages
-                                 ? P.pool.at(id, ahead.kvh, (key0 & ((1 << lg) - 1)) + copy_row) + copy_part * (16 / (int)sizeof(KVT)) : 0;
+      auto copy = [&](int row, long long src, bool real) {
+        const int bytes = real ? 16 : 0;                       // what is not there is filled with zeros: 0 times stale bits must stay 0
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pr_part<C::ROW>(row, copy_part)), "l"(kb + src), "r"(bytes) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                         dst + PR_HALF + (C::TF32 ? pr_part_v32<C::ROW>(row, copy_part) : pr_part<C::ROW>(row, copy_part))),
+                     "l"(vb + src), "r"(bytes) : "memory");
+      };
+      constexpr int PER_PART = 16 / (int)sizeof(KVT);
+      uint32_t mask;
+      if (one_page) {
+        const int id = __shfl_sync(0xffffffffu, ids, (key0 >> lg) - page0);
+        const bool ok = id >= 0 && id < P.pool.n_pages;
+        mask = !ok || left <= 0 ? 0 : left >= C::KEYS ? (C::KEYS == 32 ? 0xffffffffu : (1u << C::KEYS) - 1) : (1u << left) - 1;
+        const long long at = ok ? P.pool.at(id, ahead.kvh, (key0 & ((1 << lg) - 1)) + copy_row) + copy_part * PER_PART : 0;
 #pragma unroll
         for (int j = 0; j < C::KEYS / COPY_ROWS; ++j) {
-          const int row = j * COPY_ROWS + copy_row, bytes = (mask >> row) & 1 ? 16 : 0;
-          const long long src = bytes ? at + j * COPY_ROWS * P.pool.row_stride : 0;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pr_part<C::ROW>(row, copy_part)), "l"(kb + src), "r"(bytes) : "memory");
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                           dst + PR_HALF + (C::TF32 ? pr_part_v32<C::ROW>(row, copy_part) : pr_part<C::ROW>(row, copy_part))),
-                       "l"(vb + src), "r"(bytes) : "memory");
+          const int row = j * COPY_ROWS + copy_row;
+          const bool real = (mask >> row) & 1;
+          copy(row, real ? at + j * COPY_ROWS * P.pool.row_stride : 0, real);
         }
       } else {
+        mask = __ballot_sync(0xffffffffu, lane < C::KEYS && lane < left && ids >= 0 && ids < P.pool.n_pages);
 #pragma unroll
         for (int j = 0; j < C::KEYS / COPY_ROWS; ++j) {
-          const int row = j * COPY_ROWS + copy_row, bytes = (mask >> row) & 1 ? 16 : 0;
-          const int id = __shfl_sync(0xffffffffu, page_id, row);
-          const long long src = bytes ? P.pool.at(id, ahead.kvh, (key0 + row) & ((1 << lg) - 1)) + copy_part * (16 / (int)sizeof(KVT)) : 0;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pr_part<C::ROW>(row, copy_part)), "l"(kb + src), "r"(bytes) : "memory");
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                           dst + PR_HALF + (C::TF32 ? pr_part_v32<C::ROW>(row, copy_part) : pr_part<C::ROW>(row, copy_part))),
-                       "l"(vb + src), "r"(bytes) : "memory");
+          const int row = j * COPY_ROWS + copy_row, id = __shfl_sync(0xffffffffu, ids, row);
+          const bool real = (mask >> row) & 1;
+          copy(row, real ? P.pool.at(id, ahead.kvh, (key0 + row) & ((1 << lg) - 1)) + copy_part * PER_PART : 0, real);
         }
       }
-      if (++ahead_unit == ahead.t1) {
-        ahead_on = share.next(P, K, ahead, ahead_end);
-        ahead_end += ahead.t1 - ahead.t0;
-        ahead_unit = ahead.t0;
-        ahead_keys = ahead.keys(K);
-      }
-      if (ahead_on) look_up();
+      if (lane == 0) there[warp][slot] = mask;
+      const bool new_piece = ++ahead_unit == ahead.key_end();
+      if (new_piece) skip_empty();
+      if (ahead_on) look_up(new_piece);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");       // an empty group past the share keeps the counts uniform
   };
@@ -393,6 +422,8 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
   PagedPiece piece = ahead;
   long long piece_end = ahead_end;
   int slot = 0;
+  skip_empty();
+  if (ahead_on) look_up(true);
 #pragma unroll
   for (int s = 0; s < PR_STAGES; ++s) fetch(s);
 
@@ -457,7 +488,7 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
     RowsAcc<D> A;
     A.clear();
     const int lim0[2] = {min(n_keys, pos + g / G + 1), min(n_keys, pos + (g + 8) / G + 1)};
-    for (int i = piece.t0; i < piece.t1; ++i) {
+    for (int i = piece.key_begin(); i < piece.key_end(); ++i) {
       asm volatile("cp.async.wait_group %0;" ::"n"(PR_STAGES - 1) : "memory");
       __syncwarp();
       const int key0 = i * C::UNIT + warp * C::KEYS;

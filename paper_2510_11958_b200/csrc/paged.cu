@@ -70,12 +70,12 @@ template <typename T, typename KVT, int D>
 cudaError_t attention_launch_t(const PagedAttentionParams &P, void *scratch, int n_sms, cudaStream_t stream) {
   using C = RowsTypes<T, KVT, D>;
   const int blocks = std::min(2 * n_sms, PAGED_MAX_BLOCKS);
-  const PagedCut K{std::max(1, PR_ROWS / (P.nq / P.nkv)), C::LG_UNIT, 1, INT32_MAX};
+  const PagedCut K{std::max(1, PR_ROWS / (P.nq / P.nkv)), C::LG_UNIT, 1, INT32_MAX, PR_LEAST};
   const PagedScratch S{static_cast<PagedCutItem *>(scratch), reinterpret_cast<float *>(static_cast<PagedCutItem *>(scratch) + PAGED_MAX_BLOCKS), PR_ROWS};
   static_assert(PAGED_MAX_BLOCKS * (sizeof(PagedCutItem) + 2ull * PR_ROWS * (D + 2) * 4) <= DMTD_PAGED_ATTENTION_SCRATCH_BYTES, "scratch");
   cudaError_t e = cudaFuncSetAttribute(paged_rows_kernel<T, KVT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e == cudaSuccess) e = launch_pdl(paged_rows_kernel<T, KVT, D>, dim3(blocks), dim3(PR_THREADS), C::SMEM, stream, P, K, S);
-  if (e == cudaSuccess) e = launch_pdl(paged_merge_kernel<T, KVT, D>, dim3(blocks, PR_ROWS / 4), dim3(128), 0, stream, P, S);
+  if (e == cudaSuccess) e = launch_pdl(paged_merge_kernel<T, KVT, D>, dim3(blocks, 1), dim3(PAGED_MERGE_WARPS * 32), 0, stream, P, S);
   return e;
 }
 

@@ -28,11 +28,17 @@ __device__ __forceinline__ long long floor_sum(unsigned long long n, unsigned lo
   }
 }
 
+// x / y without the 64-bit division where 32 bits do
+__device__ __forceinline__ long long quotient(long long x, long long y) {
+  return ((x | y) >> 32) ? x / y : (long long)((unsigned)x / (unsigned)y);
+}
+
 // Which requests are on a launch's line, and how they are cut.
 struct PagedCut {
   int tile;                          // positions of a row tile
   int lg_unit;
   int min_new, max_new;              // requests of that many new rows
+  int least;                         // units of a share, at least
 };
 
 struct PagedRequest {
@@ -85,20 +91,38 @@ struct PagedPiece {
 // THREADS threads of a block work out the line's length and their block's share.
 template <int THREADS>
 struct PagedShare {
+  static constexpr int KEPT = 2 * THREADS;               // requests kept in shared memory: others are read anew where they are needed
   long long total, begin, end;
+  long long each, rest;              // a share's units: `each`, and `rest` of the shares have one more
   int n_blocks;
   struct Shared {
     long long upto[THREADS];         // units of the threads' requests up to and with a thread's own
+    int kept[KEPT][3];               // row0, n, c
   };
+  __device__ __forceinline__ PagedRequest request(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, int b) const {
+    if (P.batch.n_requests > KEPT) return paged_request(P.batch, P.pool.lg_page, K, b);
+    PagedRequest r;
+    r.b = b;
+    r.row0 = sh.kept[b][0];
+    r.n = sh.kept[b][1];
+    r.c = sh.kept[b][2];
+    r.tiles = (r.n + K.tile - 1) / K.tile;
+    return r;
+  }
 
   // Whole block; `sh` in shared memory.
   __device__ __forceinline__ void plan(const PagedAttentionParams &P, const PagedCut &K, Shared &sh, int block, int grid) {
-    const int B = P.batch.n_requests, each = (B + THREADS - 1) / THREADS, b0 = threadIdx.x * each;
+    const int B = P.batch.n_requests, per = (B + THREADS - 1) / THREADS, b0 = threadIdx.x * per;
     long long mine = 0;
     if (threadIdx.x < THREADS) {
-      for (int b = b0; b < min(B, b0 + each); ++b) {
+      for (int b = b0; b < min(B, b0 + per); ++b) {
         const PagedRequest r = paged_request(P.batch, P.pool.lg_page, K, b);
         mine += r.units_before(K, r.tiles) * P.nkv;
+        if (B <= KEPT) {
+          sh.kept[b][0] = r.row0;
+          sh.kept[b][1] = r.n;
+          sh.kept[b][2] = r.c;
+        }
       }
       // within a warp, then over the warps
 #pragma unroll
@@ -116,17 +140,18 @@ struct PagedShare {
     if (threadIdx.x < THREADS) sh.upto[threadIdx.x] = mine;
     __syncthreads();
     total = sh.upto[THREADS - 1];
-    n_blocks = (int)min((long long)grid, total);          // no empty shares: the pieces of an item are consecutive blocks
+    // no empty shares: the pieces of an item are consecutive blocks
+    n_blocks = (int)min((long long)grid, quotient(total + K.least - 1, K.least));
+    each = n_blocks ? quotient(total, n_blocks) : 0;
+    rest = total - each * n_blocks;
     begin = block < n_blocks ? start(block) : total;
     end = block < n_blocks ? start(block + 1) : total;
   }
-  __device__ __forceinline__ long long start(int block) const { return total / n_blocks * block + total % n_blocks * block / n_blocks; }
+  __device__ __forceinline__ long long start(int block) const { return each * block + min((long long)block, rest); }
   // the block that holds unit u
   __device__ __forceinline__ int holder(long long u) const {
-    int b = (int)min((long long)n_blocks - 1, u / max(1ll, total / n_blocks));
-    while (start(b) > u) --b;
-    while (start(b + 1) <= u) ++b;
-    return b;
+    const long long longer = rest * (each + 1);          // units of the longer shares, which come first
+    return (int)(u < longer ? quotient(u, each + 1) : rest + quotient(u - longer, each));
   }
 
   // The piece that begins at unit u of the line (u < end).
@@ -136,11 +161,11 @@ struct PagedShare {
       const int mid = (lo + hi) >> 1;
       if (sh.upto[mid] > u) hi = mid; else lo = mid + 1;
     }
-    const int B = P.batch.n_requests, each = (B + THREADS - 1) / THREADS;
+    const int B = P.batch.n_requests, per = (B + THREADS - 1) / THREADS;
     long long v = u - (lo ? sh.upto[lo - 1] : 0);
     PagedPiece p;
-    for (int b = lo * each;; ++b) {
-      p.r = paged_request(P.batch, P.pool.lg_page, K, b);
+    for (int b = lo * per;; ++b) {
+      p.r = request(P, K, sh, b);
       const long long all = p.r.units_before(K, p.r.tiles) * P.nkv;
       if (v < all || b + 1 >= B) break;
       v -= all;
@@ -154,20 +179,20 @@ struct PagedShare {
     v -= p.r.units_before(K, t) * P.nkv;
     p.i = t;
     p.per_item = p.r.units(K, t);
-    p.kvh = (int)(v / p.per_item);
+    p.kvh = (int)quotient(v, p.per_item);
     p.t0 = (int)(v - (long long)p.kvh * p.per_item);
     p.t1 = (int)min((long long)p.per_item, p.t0 + (end - u));
     return p;
   }
   // The piece behind p, which ends at unit u of the line; false: the share ends there.
-  __device__ __forceinline__ bool next(const PagedAttentionParams &P, const PagedCut &K, PagedPiece &p, long long u) const {
+  __device__ __forceinline__ bool next(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, PagedPiece &p, long long u) const {
     if (u >= end) return false;
     if (++p.kvh == P.nkv) {
       p.kvh = 0;
       if (++p.i == p.r.tiles) {
         p.i = 0;
         int b = p.r.b;
-        do { p.r = paged_request(P.batch, P.pool.lg_page, K, ++b); } while (p.r.n == 0 && b + 1 < P.batch.n_requests);
+        do { p.r = request(P, K, sh, ++b); } while (p.r.n == 0 && b + 1 < P.batch.n_requests);
       }
       p.per_item = p.r.units(K, p.i);
     }
@@ -197,50 +222,48 @@ struct PagedScratch {
 // A block's place for the piece of an item that began in an earlier block / that goes on in a later one.
 __device__ __forceinline__ int paged_place(int block, bool began_here) { return 2 * block + (began_here ? 1 : 0); }
 
-__device__ __forceinline__ PagedCutItem paged_cut_item(const PagedPiece &p, const PagedCut &K, int pieces) {
-  PagedCutItem c{};
-  c.pieces = pieces;
-  c.b = p.r.b;
-  c.row0 = p.r.row0 + p.first(K);
-  c.rows = p.rows(K);
-  c.first_seen = p.position(K) + 1;
-  c.kvh = p.kvh;
-  return c;
-}
-
-// grid (blocks of the attention's launch, row groups), 4 warps: block (j, y) joins rows of the item that is cut at the end of
-// block j's share.  Levels are powers of two.  A warp takes a query row at a time: its lanes fetch the pieces' levels side
-// by side, then all lanes the pieces' sums, which do not depend on each other.
+// grid (blocks of the attention's launch, row groups): block (j, y) joins rows of the item that is cut at the end of block
+// j's share.  Levels are powers of two.  A warp takes a query row at a time: its lanes fetch the pieces' levels side by
+// side, and all lanes the pieces' sums, which do not wait for the levels.
+constexpr int PAGED_MERGE_WARPS = 16;
 template <typename T, typename KVT, int D>
-__global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant__ PagedAttentionParams P, PagedScratch S) {
-  constexpr int E = D / 32;
+__global__ void __launch_bounds__(PAGED_MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ PagedAttentionParams P, PagedScratch S) {
+  constexpr int E = D / 32, DEEP = 8;
   paged_enter();
   const PagedCutItem c = S.items[blockIdx.x];
   if (c.pieces == 0) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = P.nq / P.nkv;
-  for (int qi = blockIdx.y * 4 + warp; qi < c.rows * G; qi += gridDim.y * 4) {
+  for (int qi = blockIdx.y * PAGED_MERGE_WARPS + warp; qi < c.rows * G; qi += gridDim.y * PAGED_MERGE_WARPS) {
     float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
     for (int s0 = 0; s0 < c.pieces; s0 += 32) {
+      const int n = min(32, c.pieces - s0);
+      auto place = [&](int s) { return paged_place(blockIdx.x + s0 + s, s0 + s == 0); };
       float2 ml = make_float2(-INFINITY, 0.f);
-      auto place = [&](int s) { return paged_place(blockIdx.x + s, s == 0); };
-      if (s0 + lane < c.pieces) ml = __ldcg(&S.levels<D>(place(s0 + lane))[qi]);
+      if (lane < n) ml = S.levels<D>(place(lane))[qi];
+      float v[DEEP][E];
+      auto load = [&](int first) {
+#pragma unroll
+        for (int s = 0; s < DEEP; ++s)
+          if (first + s < n) load_pack(S.sums<D>(place(first + s)) + (size_t)qi * D + lane * E, v[s]);
+      };
+      load(0);
       const float top = fmaxf(m, warp_max(ml.x));
       const float old = m > -INFINITY ? exp2f(m - top) : 0.f;
       const float w = ml.x > -INFINITY ? exp2f(ml.x - top) : 0.f;
       l = l * old + warp_sum(ml.y * w);
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] *= old;
-      const int n = min(32, c.pieces - s0);
-#pragma unroll 8
-      for (int s = 0; s < n; ++s) {
-        const float ws = __shfl_sync(0xffffffffu, w, s);
-        float v[E];
-        load_pack(S.sums<D>(place(s0 + s)) + (size_t)qi * D + lane * E, v);
-        if (ws != 0.f) {
+      for (int first = 0; first < n; first += DEEP) {
+        if (first > 0) load(first);
 #pragma unroll
-          for (int e = 0; e < E; ++e) o[e] = fmaf(ws, v[e], o[e]);
+        for (int s = 0; s < DEEP; ++s) {
+          const float ws = __shfl_sync(0xffffffffu, w, (first + s) & 31);
+          if (first + s < n && ws != 0.f) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(ws, v[s][e], o[e]);
+          }
         }
       }
       m = top;

@@ -7,10 +7,12 @@
 // 32 at a time, long before they are needed.  Pages of fewer positions than a tile has: a lane looks up each
 // key's page a tile ahead, and the lanes that copy a row ask that lane for it.
 //
-// Types.  16-bit queries: one product each for Q K^T and P V, probabilities rounded once to the cache's type, relative to
-// the largest of their own tile (which therefore is not rounded).  fp32 queries: queries and probabilities as two fp16 or three bf16
-// parts, exact to 2^-22 and 2^-24, a product per part; the cache's values are exact as they are.  fp32 cache: everything in two tf32 parts
-// (2^-22), three products.  In those forms a tile's P V is summed from zero and added to the row's sums in fp32.
+// Softmax.  A row's probabilities are relative to a reference that is raised only when a score lies more than 2^6 above it (as
+// the first one does): in between, a tile needs no maximum over the lanes and no scaling of the sums, and the exponentials do not wait for one.
+//
+// Types.  16-bit queries: one product each for Q K^T and P V, probabilities rounded once to the cache's type.  fp32
+// queries: queries and probabilities as two fp16 or three bf16 parts, exact to 2^-22 and 2^-24, a product per part; the cache's values
+// are exact as they are.  fp32 cache: everything in two tf32 parts (2^-22), three products.
 //
 // Bound: KV bytes.  An SM's share of HBM is a tile in 360 cycles; its arithmetic takes 260 (32 MMAs) with 16-bit queries.
 #pragma once
@@ -27,7 +29,27 @@ constexpr int PR_STAGES = 2;
 constexpr int PR_HALF = 4096;                                  // bytes of a tile's K, and of its V
 constexpr int PR_SLOT = 2 * PR_HALF;
 constexpr int PR_ROWS = 16;                                    // query rows of an item
-constexpr float PR_BELOW = 6.f;                                // a tile's level lies at most this far (in powers of two) below the largest score
+constexpr int PR_LEAST = 2;                                    // units of a block's share, at least: one would be an item's fixed cost alone
+constexpr float PR_ABOVE = 6.f;                                // a score may lie this far (in powers of two) above its row's reference
+
+// A piece of a block's share as the warps go through it.
+struct RowsPiece {
+  int b, row0, rows, kvh;            // request, first row of q, rows, kv head
+  int pos, keys;                     // position of the first row; keys that the last row sees (0: the piece has no units of keys)
+  int u0, u1;                        // units of keys, one at least
+  int began, ends;                   // the item begins / ends in this piece
+  int pieces;                        // of an item that goes on behind the share
+  int last;                          // the share's last piece
+};
+constexpr int PR_PIECES = 5;         // in a piece, its copies get as far as the third behind it, page ids to the fourth
+
+struct RowsShared {
+  PagedShare<PR_THREADS>::Shared line;
+  PagedPiece made;                   // the last piece made, by thread 0
+  long long made_end;                // ... its end on the line
+  RowsPiece piece[PR_PIECES];
+  uint32_t there[PR_WARPS][PR_STAGES];         // a bit per key of a ring slot
+};
 
 // Types of a launch: T queries, KVT cache.
 template <typename T, typename KVT, int D>
@@ -40,17 +62,19 @@ struct RowsTypes {
   static constexpr int COPIES = ROW / 16;                      // 16-byte parts of a row
   static constexpr int UNIT = PR_WARPS * KEYS;                 // keys of a unit of work
   static constexpr int LG_UNIT = UNIT == 32 ? 5 : UNIT == 64 ? 6 : 7;
-  // fp16 keeps its full precision down to 2^-14: probabilities are 2^10 times their size there
-  static constexpr float LIFT = std::is_same<KVT, __half>::value ? 10.f : 0.f;
-  static constexpr int QROW = ROW + 16;                        // bytes of a query row in shared memory, free of bank conflicts
-  static constexpr int Q_PARTS = TF32 ? 1 : PARTS;             // tf32: the first part lives in registers
+  // fp16 keeps its full precision down to 2^-14 and ends at 2^16: probabilities are 2^8 times their size there
+  static constexpr float LIFT = std::is_same<KVT, __half>::value ? 8.f : 0.f;
+  static constexpr int RAW_ROW = D * (int)sizeof(T) + 16;      // bytes of a query row as it comes; free of bank conflicts
+  static constexpr int QROW = ROW + 16;                        // ... of its parts
+  static constexpr int Q_PARTS = TF32 ? 1 : PARTS > 1 ? PARTS : 0;      // one part: taken from the rows as they come; tf32: the first is in registers
   static constexpr int OROW = D + 8;
-  static constexpr int Q = PR_WARPS * PR_STAGES * PR_SLOT;
-  static constexpr int OS = Q + Q_PARTS * PR_ROWS * QROW;
+  static constexpr int RAW = PR_WARPS * PR_STAGES * PR_SLOT;
+  static constexpr int OS = RAW + PR_ROWS * RAW_ROW;           // the warps' outputs, over the queries' parts
+  static constexpr int Q = OS;
   static constexpr int RED = OS + PR_WARPS * PR_ROWS * OROW * 4;
   static constexpr int SMEM = RED + 2 * PR_WARPS * PR_ROWS * 4;
-  static_assert(2 * (SMEM + 1024 + 64) <= 228 * 1024, "two blocks per SM");
-  static_assert(sizeof(typename PagedShare<PR_THREADS>::Shared) <= RED - OS, "the line's sums lie where the outputs are put later");
+  static_assert(Q_PARTS * PR_ROWS * QROW <= RED - OS, "parts of the queries");
+  static_assert(2 * (SMEM + 1024 + (int)sizeof(RowsShared)) <= 228 * 1024, "two blocks per SM");
 };
 
 // byte offset of 16-byte part `part` of row `row` in a tile: conflict-free for the copies, for the 16-byte operand loads of K
@@ -95,10 +119,10 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&p)[N]) {
 // tf32: n-tile 4 blk + j holds dimensions 32 blk + 8 t + j, + 4.
 template <int D>
 struct RowsAcc {
-  float m[2], l[2], top[2];          // per row: level of the sums (powers of two), this lane's share of the sum, largest score
+  float m[2], l[2];                  // per row: level of the sums (powers of two), this lane's share of the sum
   float o[D / 8][4];
   __device__ __forceinline__ void clear() {
-    m[0] = m[1] = top[0] = top[1] = -INFINITY;
+    m[0] = m[1] = -INFINITY;
     l[0] = l[1] = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -193,30 +217,38 @@ __device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t 
       }
     }
   }
-  float corr[2];
+  float mx[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    float mx = fmaxf(c[0][2 * h], c[0][2 * h + 1]);
+    mx[h] = fmaxf(c[0][2 * h], c[0][2 * h + 1]);
 #pragma unroll
-    for (int j = 1; j < NT; ++j) mx = fmaxf(mx, fmaxf(c[j][2 * h], c[j][2 * h + 1]));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-    A.top[h] = fmaxf(A.top[h], mx);
-    const float level = fmaxf(mx, A.top[h] - PR_BELOW) - C::LIFT;
-    corr[h] = level > -INFINITY ? exp2_approx(A.m[h] - level) : 1.f;
-    A.m[h] = level;
+    for (int j = 1; j < NT; ++j) mx[h] = fmaxf(mx[h], fmaxf(c[j][2 * h], c[j][2 * h + 1]));
   }
-  float sum[2] = {0.f, 0.f};
+  if (__any_sync(0xffffffffu, mx[0] > A.m[0] + (PR_ABOVE + C::LIFT) || mx[1] > A.m[1] + (PR_ABOVE + C::LIFT))) {
+    float f[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
+      mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
+      const float level = fmaxf(mx[h] - C::LIFT, A.m[h]);
+      f[h] = level > -INFINITY ? exp2_approx(A.m[h] - level) : 1.f;
+      A.m[h] = level;
+      A.l[h] *= f[h];
+    }
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      A.o[i][0] *= f[0]; A.o[i][1] *= f[0]; A.o[i][2] *= f[1]; A.o[i][3] *= f[1];
+    }
+  }
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      c[j][e] = c[j][e] == -INFINITY ? 0.f : exp2_approx(c[j][e] - A.m[e >> 1]);       // (NaN stays)
-      sum[e >> 1] += c[j][e];
+      // (a row without any key so far has no reference; NaN stays)
+      c[j][e] = c[j][e] == -INFINITY ? 0.f : exp2_approx(c[j][e] - A.m[e >> 1]);
+      A.l[e >> 1] += c[j][e];
     }
   }
-  A.l[0] = A.l[0] * corr[0] + sum[0];
-  A.l[1] = A.l[1] * corr[1] + sum[1];
   if constexpr (C::TF32) {
     // column k = t of the A operand is key 2 t, column t + 4 key 2 t + 1
     uint32_t ph[NT][4], pl[NT][4];
@@ -229,12 +261,6 @@ __device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t 
     }
 #pragma unroll
     for (int blk = 0; blk < D / 32; ++blk) {
-      float s[4][4], lo[4][4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-        lo[i][0] = lo[i][1] = lo[i][2] = lo[i][3] = 0.f;
-      }
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
         const uint4 v0 = lds128(v_t + pr_part_v32<C::ROW>(j * 8 + 2 * t, blk * 8 + g));
@@ -245,15 +271,11 @@ __device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t 
           uint32_t ah, al, bh, bl;
           tf32_split(__uint_as_float(a[i]), ah, al);
           tf32_split(__uint_as_float(b[i]), bh, bl);
-          mma_tf32_1688(s[i], ph[j][0], ph[j][1], ph[j][2], ph[j][3], ah, bh);
-          mma_tf32_1688(lo[i], ph[j][0], ph[j][1], ph[j][2], ph[j][3], al, bl);
-          mma_tf32_1688(lo[i], pl[j][0], pl[j][1], pl[j][2], pl[j][3], ah, bh);
+          float(&o)[4] = A.o[blk * 4 + i];
+          mma_tf32_1688(o, ph[j][0], ph[j][1], ph[j][2], ph[j][3], al, bl);
+          mma_tf32_1688(o, pl[j][0], pl[j][1], pl[j][2], pl[j][3], ah, bh);
+          mma_tf32_1688(o, ph[j][0], ph[j][1], ph[j][2], ph[j][3], ah, bh);
         }
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) A.o[blk * 4 + i][e] = fmaf(A.o[blk * 4 + i][e], corr[e >> 1], s[i][e] + lo[i][e]);
       }
     }
   } else {
@@ -267,40 +289,14 @@ __device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t 
     const int mi = lane >> 3, rr = (mi & 1) * 8 + (lane & 7);
 #pragma unroll
     for (int d2 = 0; d2 < D / 16; ++d2) {
-      if constexpr (C::PARTS == 1) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float(&o)[4] = A.o[2 * d2 + h];
-          o[0] *= corr[0]; o[1] *= corr[0]; o[2] *= corr[1]; o[3] *= corr[1];
-        }
+      for (int ks = 0; ks < KS; ++ks) {
+        uint32_t b0, b1, b2, b3;
+        ldmatrix_x4_trans(v_t + pr_part<C::ROW>(ks * 16 + rr, d2 * 2 + (mi >> 1)), b0, b1, b2, b3);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          uint32_t b0, b1, b2, b3;
-          ldmatrix_x4_trans(v_t + pr_part<C::ROW>(ks * 16 + rr, d2 * 2 + (mi >> 1)), b0, b1, b2, b3);
-          Op::mma(A.o[2 * d2], p[ks][0][0], p[ks][1][0], p[ks][2][0], p[ks][3][0], b0, b1);
-          Op::mma(A.o[2 * d2 + 1], p[ks][0][0], p[ks][1][0], p[ks][2][0], p[ks][3][0], b2, b3);
-        }
-      } else {
-        float s[2][4], lo[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          s[h][0] = s[h][1] = s[h][2] = s[h][3] = 0.f;
-          lo[h][0] = lo[h][1] = lo[h][2] = lo[h][3] = 0.f;
-        }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          uint32_t b0, b1, b2, b3;
-          ldmatrix_x4_trans(v_t + pr_part<C::ROW>(ks * 16 + rr, d2 * 2 + (mi >> 1)), b0, b1, b2, b3);
-#pragma unroll
-          for (int part = 0; part < C::PARTS; ++part) {
-            Op::mma(part ? lo[0] : s[0], p[ks][0][part], p[ks][1][part], p[ks][2][part], p[ks][3][part], b0, b1);
-            Op::mma(part ? lo[1] : s[1], p[ks][0][part], p[ks][1][part], p[ks][2][part], p[ks][3][part], b2, b3);
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) A.o[2 * d2 + h][e] = fmaf(A.o[2 * d2 + h][e], corr[e >> 1], s[h][e] + lo[h][e]);
+        for (int part = C::PARTS - 1; part >= 0; --part) {
+          Op::mma(A.o[2 * d2], p[ks][0][part], p[ks][1][part], p[ks][2][part], p[ks][3][part], b0, b1);
+          Op::mma(A.o[2 * d2 + 1], p[ks][0][part], p[ks][1][part], p[ks][2][part], p[ks][3][part], b2, b3);
         }
       }
     }
@@ -312,75 +308,100 @@ struct RowsQueries {                 // what of the queries is in registers: all
   uint4 v[C::TF32 ? D / 16 : D / 32][2];
 };
 
+// Thread 0: `p`, which ends at unit `end` of the line, as the warps need it.
+__device__ __forceinline__ void rows_describe(RowsPiece &d, const PagedPiece &p, long long end, const PagedCut &K, const PagedShare<PR_THREADS> &share) {
+  const bool any = p.key_end() > p.key_begin();
+  d.b = p.r.b;
+  d.row0 = p.r.row0 + p.first(K);
+  d.rows = p.rows(K);
+  d.kvh = p.kvh;
+  d.pos = p.position(K);
+  d.keys = any ? p.keys(K) : 0;
+  d.u0 = any ? p.key_begin() : 0;
+  d.u1 = any ? p.key_end() : 1;
+  d.began = p.t0 == 0;
+  d.ends = p.t1 == p.per_item;
+  d.last = end >= share.end;
+  d.pieces = d.last && d.began && !d.ends ? share.holder(end - 1 + (p.per_item - p.t1)) - (int)blockIdx.x + 1 : 0;
+}
+
 template <typename T, typename KVT, int D>
 __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_constant__ PagedAttentionParams P, PagedCut K, PagedScratch S) {
   using C = RowsTypes<T, KVT, D>;
   using Op = typename std::conditional<std::is_same<KVT, __half>::value, OpF16, OpBf16>::type;
   extern __shared__ __align__(128) unsigned char sc[];
-  auto &line = *reinterpret_cast<typename PagedShare<PR_THREADS>::Shared *>(sc + C::OS);
-  __shared__ uint32_t there[PR_WARPS][PR_STAGES];              // a bit per key of a ring slot
+  __shared__ RowsShared sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int G = P.nq / P.nkv, lg = P.pool.lg_page;
+  const uint32_t g_inv = (65536 + G - 1) / G;                  // i / G == i * g_inv >> 16 for i < 16
   paged_enter();
   PagedShare<PR_THREADS> share;
-  share.plan(P, K, line, blockIdx.x, gridDim.x);
+  share.plan(P, K, sh.line, blockIdx.x, gridDim.x);
   if (share.begin >= share.end) {
     if (threadIdx.x == 0) S.items[blockIdx.x].pieces = 0;
     return;
   }
-  const uint32_t ring = smem_u32(sc) + warp * PR_STAGES * PR_SLOT, q_t = smem_u32(sc) + C::Q;
+  // thread 0 keeps the list of pieces five ahead, so that what a piece looks at was made before a barrier
+  auto make_piece = [&](int index) {
+    PagedPiece p = sh.made;
+    long long end = sh.made_end;
+    if (!share.next(P, K, sh.line, p, end)) return;
+    end += p.t1 - p.t0;
+    rows_describe(sh.piece[index % PR_PIECES], p, end, K, share);
+    sh.made = p;
+    sh.made_end = end;
+  };
+  if (threadIdx.x == 0) {
+    sh.made = share.find(P, K, sh.line, share.begin);
+    sh.made_end = share.begin + (sh.made.t1 - sh.made.t0);
+    rows_describe(sh.piece[0], sh.made, sh.made_end, K, share);
+    for (int i = 1; i < PR_PIECES; ++i) make_piece(i);
+  }
+  __syncthreads();
+  const uint32_t ring = smem_u32(sc) + warp * PR_STAGES * PR_SLOT, raw_t = smem_u32(sc) + C::RAW, q_t = smem_u32(sc) + C::Q;
   float *const o_s = reinterpret_cast<float *>(sc + C::OS), *const red_m = reinterpret_cast<float *>(sc + C::RED);
   float *const red_l = red_m + PR_WARPS * PR_ROWS;
   const float scale = 1.4426950408889634f * rsqrtf((float)D);
   const KVT *const kb = reinterpret_cast<const KVT *>(P.pool.k), *const vb = reinterpret_cast<const KVT *>(P.pool.v);
 
-  // ---- the copies' place on the line: the piece, its next unit of keys, the page ids at hand
-  PagedPiece ahead = share.find(P, K, line, share.begin);
-  long long ahead_end = share.begin + (ahead.t1 - ahead.t0);   // of the piece, on the line
-  int ahead_unit = ahead.key_begin(), ahead_keys = ahead.keys(K);
-  bool ahead_on = true;
+  // ---- the copies' place: the piece, its next unit of keys, the page ids at hand
   const int copy_part = lane % C::COPIES, copy_row = lane / C::COPIES;
   constexpr int COPY_ROWS = 32 / C::COPIES;                    // rows of one instruction
   constexpr int LG_KEYS = C::KEYS == 8 ? 3 : C::KEYS == 16 ? 4 : 5;
   const bool one_page = lg >= LG_KEYS;                         // a tile lies in one page
+  int ahead = 0, ahead_unit, ahead_end, ahead_keys, ahead_kvh, ahead_last;
+  const int *ahead_table;
   // one_page: lane i has the id of page page0 + i, and once they are asked for of page page0 + 32 + i; else lane i has that
-  // of the page of the next tile's key i
-  int ids = -1, ids_next = -1, page0 = 0;
+  // of the page of the next tile's key i.  first_ids: the same for the first tile of the piece behind
+  int ids = -1, ids_next = -1, page0 = 0, first_ids = -1;
   bool asked = false;
-  auto page_at = [&](int page) {
-    return ((long long)page << lg) < ahead_keys ? P.batch.table[(size_t)ahead.r.b * P.batch.table_stride + page] : -1;
+  auto page_of = [&](const int *table, int keys, int page) { return ((long long)page << lg) < keys ? table[page] : -1; };
+  auto table_of = [&](int b) { return P.batch.table + (size_t)b * P.batch.table_stride; };
+  auto first_page = [&](int unit) {                            // this lane's page at the first tile of a piece
+    const int key = unit * C::UNIT + warp * C::KEYS;
+    return one_page ? (key >> lg) + lane : (key + (lane & (C::KEYS - 1))) >> lg;
   };
-  auto tile_key = [&]() { return ahead_unit * C::UNIT + warp * C::KEYS; };
-  auto look_up = [&](bool new_piece) {
-    if (!one_page) {
-      ids = page_at((tile_key() + (lane & (C::KEYS - 1))) >> lg);
-      return;
-    }
-    const int page = tile_key() >> lg;
-    if (new_piece) {
-      page0 = page;
-      ids = page_at(page0 + lane);
-      asked = false;
-    } else if (page - page0 >= 32) {                           // (a unit spans four pages at most)
-      page0 += 32;
-      ids = ids_next;
-      asked = false;
-    } else if (page - page0 >= 16 && !asked) {
-      ids_next = page_at(page0 + 32 + lane);
-      asked = true;
-    }
+  auto ask_first = [&](int index) {
+    const RowsPiece &d = sh.piece[index % PR_PIECES];
+    first_ids = page_of(table_of(d.b), d.keys, first_page(d.u0));
   };
-  auto skip_empty = [&]() {                                    // pieces without keys have no copies
-    while (ahead_on && ahead_unit >= ahead.key_end()) {
-      ahead_on = share.next(P, K, ahead, ahead_end);
-      ahead_end += ahead.t1 - ahead.t0;
-      ahead_unit = ahead.key_begin();
-      ahead_keys = ahead.keys(K);
-    }
+  auto enter_piece = [&](int index) {                          // its first ids are in first_ids
+    const RowsPiece &d = sh.piece[index % PR_PIECES];
+    ahead_unit = d.u0;
+    ahead_end = d.u1;
+    ahead_keys = d.keys;
+    ahead_kvh = d.kvh;
+    ahead_last = d.last;
+    ahead_table = table_of(d.b);
+    page0 = (ahead_unit * C::UNIT + warp * C::KEYS) >> lg;
+    ids = first_ids;
+    asked = false;
+    if (!ahead_last) ask_first(index + 1);
   };
+  bool ahead_on = true;
   auto fetch = [&](int slot) {
     if (ahead_on) {
-      const int key0 = tile_key(), left = ahead_keys - key0;  // keys from the tile's first on
+      const int key0 = ahead_unit * C::UNIT + warp * C::KEYS, left = ahead_keys - key0;      // left: keys from the tile's first on
       const uint32_t dst = ring + slot * PR_SLOT;
       auto copy = [&](int row, long long src, bool real) {
         const int bytes = real ? 16 : 0;                       // what is not there is filled with zeros: 0 times stale bits must stay 0
@@ -395,7 +416,7 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
         const int id = __shfl_sync(0xffffffffu, ids, (key0 >> lg) - page0);
         const bool ok = id >= 0 && id < P.pool.n_pages;
         mask = !ok || left <= 0 ? 0 : left >= C::KEYS ? (C::KEYS == 32 ? 0xffffffffu : (1u << C::KEYS) - 1) : (1u << left) - 1;
-        const long long at = ok ? P.pool.at(id, ahead.kvh, (key0 & ((1 << lg) - 1)) + copy_row) + copy_part * PER_PART : 0;
+        const long long at = ok ? P.pool.at(id, ahead_kvh, (key0 & ((1 << lg) - 1)) + copy_row) + copy_part * PER_PART : 0;
 #pragma unroll
         for (int j = 0; j < C::KEYS / COPY_ROWS; ++j) {
           const int row = j * COPY_ROWS + copy_row;
@@ -408,96 +429,116 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
         for (int j = 0; j < C::KEYS / COPY_ROWS; ++j) {
           const int row = j * COPY_ROWS + copy_row, id = __shfl_sync(0xffffffffu, ids, row);
           const bool real = (mask >> row) & 1;
-          copy(row, real ? P.pool.at(id, ahead.kvh, (key0 + row) & ((1 << lg) - 1)) + copy_part * PER_PART : 0, real);
+          copy(row, real ? P.pool.at(id, ahead_kvh, (key0 + row) & ((1 << lg) - 1)) + copy_part * PER_PART : 0, real);
         }
       }
-      if (lane == 0) there[warp][slot] = mask;
-      const bool new_piece = ++ahead_unit == ahead.key_end();
-      if (new_piece) skip_empty();
-      if (ahead_on) look_up(new_piece);
+      if (lane == 0) sh.there[warp][slot] = mask;
+      // the next tile, and its page ids
+      if (++ahead_unit == ahead_end) {
+        if (ahead_last) ahead_on = false;
+        else enter_piece(++ahead);
+      } else if (!one_page) {
+        ids = page_of(ahead_table, ahead_keys, first_page(ahead_unit));
+      } else {
+        const int page = (ahead_unit * C::UNIT + warp * C::KEYS) >> lg;          // (a unit spans four pages at most)
+        if (page - page0 >= 32) {
+          page0 += 32;
+          ids = ids_next;
+          asked = false;
+        } else if (page - page0 >= 16 && !asked) {
+          ids_next = page_of(ahead_table, ahead_keys, page0 + 32 + lane);
+          asked = true;
+        }
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");       // an empty group past the share keeps the counts uniform
   };
-
-  PagedPiece piece = ahead;
-  long long piece_end = ahead_end;
-  int slot = 0;
-  skip_empty();
-  if (ahead_on) look_up(true);
+  // a piece's query rows as they are: row qi = (row row0 + qi / G, head kvh * G + qi % G); beyond the tile's rows zero
+  auto fetch_queries = [&](int index) {
+    const RowsPiece &d = sh.piece[index % PR_PIECES];
+    constexpr int PER_ROW = D * (int)sizeof(T) / 16;
+    const T *q = reinterpret_cast<const T *>(P.q);
 #pragma unroll
+    for (int k = 0; k < PR_ROWS * PER_ROW / PR_THREADS; ++k) {
+      const int idx = threadIdx.x + k * PR_THREADS, qi = idx / PER_ROW, part = idx % PER_ROW, r = qi * g_inv >> 16;
+      const bool real = r < d.rows;
+      const T *src = real ? q + (d.row0 + r) * P.q_stride + (d.kvh * G + qi - r * G) * D + part * (16 / (int)sizeof(T)) : q;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(raw_t + qi * C::RAW_ROW + part * 16), "l"(src), "r"(real ? 16 : 0) : "memory");
+    }
+  };
+  fetch_queries(0);                                            // (part of the first tile's group)
+  ask_first(0);
+  enter_piece(0);
+#pragma unroll 1
   for (int s = 0; s < PR_STAGES; ++s) fetch(s);
 
-  for (;;) {
-    const int rows = piece.rows(K), nQ = rows * G, n_keys = piece.keys(K), pos = piece.position(K);
-    const int row0 = piece.r.row0 + piece.first(K);
-    // ---- queries: row qi = (row row0 + qi / G, head kvh * G + qi % G); beyond nQ zero
-    for (int idx = threadIdx.x; idx < PR_ROWS * (D / 8); idx += PR_THREADS) {
-      const int qi = idx / (D / 8), d = idx % (D / 8) * 8;
-      float f[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = 0.f;
-      if (qi < nQ) load_pack(reinterpret_cast<const T *>(P.q) + (row0 + qi / G) * P.q_stride + (piece.kvh * G + qi % G) * D + d, f);
-      if constexpr (C::TF32) {
-        float *dst = reinterpret_cast<float *>(sc + C::Q + qi * C::QROW) + d;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dst[j] = f[j];
-      } else {
-        uint32_t w[4][C::PARTS];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) split_pair<Op, C::PARTS>(f[2 * j], f[2 * j + 1], w[j]);
-#pragma unroll
-        for (int part = 0; part < C::PARTS; ++part)
-          sts128(q_t + (part * PR_ROWS + qi) * C::QROW + d * 2, make_uint4(w[0][part], w[1][part], w[2][part], w[3][part]));
-      }
-    }
-    __syncthreads();
+  int slot = 0;
+  bool q_behind = false;                                       // this piece's queries may be in the newest group of copies
+  for (int index = 0;; ++index) {
+    const RowsPiece d = sh.piece[index % PR_PIECES];
+    const int nQ = d.rows * G;
+    // ---- queries
+    if (q_behind) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    else asm volatile("cp.async.wait_group %0;" ::"n"(PR_STAGES - 1) : "memory");
+    __syncthreads();                                           // ... of every thread; the outputs before them have been read
     RowsQueries<C, D> qh;
     if constexpr (C::TF32) {
-      // the first parts to registers; what remains takes their place
+      // the first parts in registers, the second ones to shared memory by one warp
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint4 x = lds128(q_t + (g + 8 * h) * C::QROW + k * 64 + t * 16);
-          qh.v[k][h] = make_uint4(tf32_of(__uint_as_float(x.x)), tf32_of(__uint_as_float(x.y)), tf32_of(__uint_as_float(x.z)), tf32_of(__uint_as_float(x.w)));
+          const uint4 x = lds128(raw_t + (g + 8 * h) * C::RAW_ROW + k * 64 + t * 16);
+          uint4 &y = qh.v[k][h];
+          uint4 z;
+          tf32_split(__uint_as_float(x.x), y.x, z.x);
+          tf32_split(__uint_as_float(x.y), y.y, z.y);
+          tf32_split(__uint_as_float(x.z), y.z, z.z);
+          tf32_split(__uint_as_float(x.w), y.w, z.w);
+          if (warp == (k & 3)) sts128(q_t + (g + 8 * h) * C::QROW + k * 64 + t * 16, z);
         }
       }
-      __syncthreads();
-      if (warp == 0) {
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t at = q_t + (g + 8 * h) * C::QROW + k * 64 + t * 16;
-            const uint4 x = lds128(at), y = qh.v[k][h];
-            sts128(at, make_uint4(tf32_of(__uint_as_float(x.x) - __uint_as_float(y.x)), tf32_of(__uint_as_float(x.y) - __uint_as_float(y.y)),
-                                  tf32_of(__uint_as_float(x.z) - __uint_as_float(y.z)), tf32_of(__uint_as_float(x.w) - __uint_as_float(y.w))));
-          }
-        }
-      }
-      __syncthreads();
     } else if constexpr (C::PARTS == 1) {
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) {
-        qh.v[k][0] = lds128(q_t + g * C::QROW + k * 64 + t * 16);
-        qh.v[k][1] = lds128(q_t + (g + 8) * C::QROW + k * 64 + t * 16);
+        qh.v[k][0] = lds128(raw_t + g * C::RAW_ROW + k * 64 + t * 16);
+        qh.v[k][1] = lds128(raw_t + (g + 8) * C::RAW_ROW + k * 64 + t * 16);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < PR_ROWS * D / 8 / PR_THREADS; ++k) {
+        const int idx = threadIdx.x + k * PR_THREADS, qi = idx / (D / 8), at = idx % (D / 8);
+        const uint4 x = lds128(raw_t + qi * C::RAW_ROW + at * 32), y = lds128(raw_t + qi * C::RAW_ROW + at * 32 + 16);
+        uint32_t w[4][C::PARTS];
+        split_pair<Op, C::PARTS>(__uint_as_float(x.x), __uint_as_float(x.y), w[0]);
+        split_pair<Op, C::PARTS>(__uint_as_float(x.z), __uint_as_float(x.w), w[1]);
+        split_pair<Op, C::PARTS>(__uint_as_float(y.x), __uint_as_float(y.y), w[2]);
+        split_pair<Op, C::PARTS>(__uint_as_float(y.z), __uint_as_float(y.w), w[3]);
+#pragma unroll
+        for (int part = 0; part < C::PARTS; ++part)
+          sts128(q_t + (part * PR_ROWS + qi) * C::QROW + at * 16, make_uint4(w[0][part], w[1][part], w[2][part], w[3][part]));
       }
     }
+    __syncthreads();                                           // parts written, rows as they came and this piece's place read
+    if (!d.last) fetch_queries(index + 1);                     // (part of the next tile's group)
+    q_behind = d.u1 - d.u0 < 2;
+    if (threadIdx.x == 0) make_piece(index + PR_PIECES);
 
     // ---- keys
     RowsAcc<D> A;
     A.clear();
-    const int lim0[2] = {min(n_keys, pos + g / G + 1), min(n_keys, pos + (g + 8) / G + 1)};
-    for (int i = piece.key_begin(); i < piece.key_end(); ++i) {
+    const int lim0[2] = {min(d.keys, d.pos + (int)(g * g_inv >> 16) + 1), min(d.keys, d.pos + (int)((g + 8) * g_inv >> 16) + 1)};
+#pragma unroll 1
+    for (int i = d.u0; i < d.u1; ++i) {
       asm volatile("cp.async.wait_group %0;" ::"n"(PR_STAGES - 1) : "memory");
       __syncwarp();
       const int key0 = i * C::UNIT + warp * C::KEYS;
       const uint32_t k_t = ring + slot * PR_SLOT;
-      if (key0 < n_keys) {
-        const uint32_t good = there[warp][slot];
+      if (key0 < d.keys) {
+        const uint32_t good = sh.there[warp][slot];
         const int lim[2] = {lim0[0] - key0, lim0[1] - key0};
         rows_tile<C, KVT, D>(A, k_t, k_t + PR_HALF, q_t, qh, scale, lim, good,
-                             key0 + C::KEYS > pos + 1 || good != (C::KEYS == 32 ? 0xffffffffu : (1u << C::KEYS) - 1));
+                             key0 + C::KEYS > d.pos + 1 || good != (C::KEYS == 32 ? 0xffffffffu : (1u << C::KEYS) - 1));
       }
       __syncwarp();                                            // the slot is free
       fetch(slot);
@@ -505,6 +546,7 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
     }
 
     // ---- the warps' results to shared memory, joined there
+    if (C::Q_PARTS) __syncthreads();                           // they lie over the queries' parts
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float l = A.l[h];
@@ -526,11 +568,11 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
       }
     }
     __syncthreads();
-    const bool whole = piece.whole();
-    const int place = paged_place(blockIdx.x, piece.t0 == 0);
+    const bool whole = d.began && d.ends;
+    const int place = paged_place(blockIdx.x, d.began);
     bool good = true;
     for (int idx = threadIdx.x; idx < nQ * (D / 4); idx += PR_THREADS) {
-      const int qi = idx / (D / 4), d = idx % (D / 4) * 4;
+      const int qi = idx / (D / 4), at = idx % (D / 4) * 4, r = qi * g_inv >> 16;
       float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < PR_WARPS; ++w) m = fmaxf(m, red_m[w * PR_ROWS + qi]);
@@ -539,40 +581,36 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
         const float mw = red_m[w * PR_ROWS + qi];
         if (mw > -INFINITY) {                                  // (a warp without keys has none)
           const float f = exp2_approx(mw - m);
-          const float4 v = *reinterpret_cast<const float4 *>(o_s + (w * PR_ROWS + qi) * C::OROW + d);
+          const float4 v = *reinterpret_cast<const float4 *>(o_s + (w * PR_ROWS + qi) * C::OROW + at);
           l = fmaf(red_l[w * PR_ROWS + qi], f, l);
           acc[0] = fmaf(v.x, f, acc[0]); acc[1] = fmaf(v.y, f, acc[1]); acc[2] = fmaf(v.z, f, acc[2]); acc[3] = fmaf(v.w, f, acc[3]);
         }
       }
       if (whole) {
+        const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          acc[j] = l != 0.f ? acc[j] / l : 0.f;
+          acc[j] = l != 0.f ? acc[j] * inv : 0.f;
           good = good && isfinite(acc[j]);
         }
-        store_pack(reinterpret_cast<T *>(P.out) + ((size_t)(row0 + qi / G) * P.nq + piece.kvh * G + qi % G) * D + d, acc);
+        store_pack(reinterpret_cast<T *>(P.out) + ((size_t)(d.row0 + r) * P.nq + d.kvh * G + qi - r * G) * D + at, acc);
       } else {
-        store_pack(S.sums<D>(place) + (size_t)qi * D + d, acc);
-        if (d == 0) S.levels<D>(place)[qi] = make_float2(m, l);
+        store_pack(S.sums<D>(place) + (size_t)qi * D + at, acc);
+        if (at == 0) S.levels<D>(place)[qi] = make_float2(m, l);
       }
     }
     // A row that is not finite: a probability of zero may have met an infinity or a NaN in a row of V that it does not see
     // (a later one of the same tile).  Such tiles are worked out again row by row.
-    if (__syncthreads_or(rows > 1 && !good)) {
-      for (int qi = warp; qi < nQ; qi += PR_WARPS)
-        paged_attend_row<T, KVT, D>(P, piece.r.b, row0 + qi / G, pos + qi / G + 1, piece.kvh * G + qi % G);
-    }
-    const bool cut_behind = piece.t0 == 0 && !whole;
-    if (piece_end >= share.end) {
-      if (threadIdx.x == 0) {
-        // the item goes on for per_item - t1 units behind the share
-        const int pieces = cut_behind ? share.holder(piece_end - 1 + (piece.per_item - piece.t1)) - (int)blockIdx.x + 1 : 0;
-        S.items[blockIdx.x] = paged_cut_item(piece, K, pieces);
+    if (d.rows > 1 && __syncthreads_or(!good)) {
+      for (int qi = warp; qi < nQ; qi += PR_WARPS) {
+        const int r = qi * g_inv >> 16;
+        paged_attend_row<T, KVT, D>(P, d.b, d.row0 + r, d.pos + r + 1, d.kvh * G + qi - r * G);
       }
+    }
+    if (d.last) {
+      if (threadIdx.x == 0) S.items[blockIdx.x] = PagedCutItem{d.pieces, d.b, d.row0, d.rows, d.pos + 1, d.kvh, {0, 0}};
       break;
     }
-    share.next(P, K, piece, piece_end);
-    piece_end += piece.t1 - piece.t0;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
 }

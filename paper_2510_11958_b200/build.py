@@ -13,7 +13,7 @@ SOURCES = ["engine.cu", "paged.cu"]
 HEADERS = ["common.cuh", "ptx.cuh", "kernels.cuh", "pass_common.cuh", "pass_stream.cuh", "pass_prologues.cuh",
            "pass_attention.cuh", "pass_attention_f32.cuh", "pass_kernel.cuh", "attention_kernel.cuh", "attention_tc05.cuh",
            "gemm_tc05.cuh", "small_pass.cuh", "host.h", "paged_common.cuh", "paged_plan.cuh", "paged_append.cuh", "paged_attention.cuh", "paged_line.cuh",
-           "paged_rows.cuh"]
+           "paged_rows.cuh", "paged_chunk.cuh"]
 
 
 def _stale() -> bool:

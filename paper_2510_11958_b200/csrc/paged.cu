@@ -6,7 +6,7 @@
 #include "host.h"
 #include "paged_append.cuh"
 #include "paged_plan.cuh"
-#include "paged_rows.cuh"
+#include "paged_chunk.cuh"
 
 using namespace dmtd;
 
@@ -16,8 +16,6 @@ dmtd_status launched(cudaError_t e, const char *what) {
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? DMTD_OK : call_failed(DMTD_ERR_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
 }
-
-constexpr int PAGED_MAX_BLOCKS = 304;                    // blocks of an attention launch, as far as scratch has places
 
 size_t dtype_bytes(int t) { return t == DMTD_F32 ? 4 : 2; }
 bool known_dtype(int t) { return t == DMTD_F32 || t == DMTD_BF16 || t == DMTD_F16; }
@@ -66,26 +64,65 @@ int sm_count() {
   return n;
 }
 
+// Scratch: the places of the row kernel's blocks, then those of the chunk kernel's.
+constexpr int ROWS_BLOCKS = 304, CHUNK_BLOCKS = 152;
+constexpr size_t scratch_part(int blocks, int rows) { return (blocks * (sizeof(PagedCutItem) + 2ull * rows * 130 * 4) + 255) / 256 * 256; }
+static_assert(scratch_part(ROWS_BLOCKS, PR_ROWS) + scratch_part(CHUNK_BLOCKS, PC_ROWS) <= DMTD_PAGED_ATTENTION_SCRATCH_BYTES, "scratch");
+PagedScratch scratch_at(void *scratch, size_t offset, int blocks, int rows) {
+  PagedCutItem *items = reinterpret_cast<PagedCutItem *>(static_cast<unsigned char *>(scratch) + offset);
+  return PagedScratch{items, reinterpret_cast<float *>(items + blocks), rows};
+}
+
+// Requests with at least this many query rows to a kv head go to the chunk kernel.
+constexpr int CHUNK_LEAST_ROWS = 65;
+
+template <typename T, int D>
+cudaError_t chunk_launch(const PagedAttentionParams &P, int min_new, void *scratch, int n_sms, cudaStream_t stream) {
+  using C = ChunkTypes<D>;
+  const auto kernel = paged_chunk_kernel<T, D>;
+  const int G = P.nq / P.nkv, blocks = std::min(n_sms, CHUNK_BLOCKS);
+  // the warpgroups' shares are taken out of the registers that the block was launched with: with fewer they would wait for ever
+  static const bool enough = [&] {
+    cudaFuncAttributes a;
+    return cudaFuncGetAttributes(&a, kernel) == cudaSuccess && a.numRegs >= 168;
+  }();
+  if (!enough) return cudaErrorInvalidConfiguration;
+  cudaError_t e;
+  const PagedCut K{PC_ROWS / G, PC_LG_TK, min_new, INT32_MAX, 2};
+  const PagedScratch S = scratch_at(scratch, scratch_part(ROWS_BLOCKS, PR_ROWS), CHUNK_BLOCKS, PC_ROWS);
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(blocks), dim3(PC_THREADS), C::SMEM, stream, P, K, S);
+  if (e == cudaSuccess) e = launch_pdl(paged_merge_kernel<T, T, D>, dim3(blocks, PC_ROWS / PAGED_MERGE_WARPS), dim3(PAGED_MERGE_WARPS * 32), 0, stream, P, S);
+  return e;
+}
+
 template <typename T, typename KVT, int D>
-cudaError_t attention_launch_t(const PagedAttentionParams &P, void *scratch, int n_sms, cudaStream_t stream) {
+cudaError_t attention_launch_t(const PagedAttentionParams &P, int max_new, void *scratch, int n_sms, cudaStream_t stream) {
   using C = RowsTypes<T, KVT, D>;
-  const int blocks = std::min(2 * n_sms, PAGED_MAX_BLOCKS);
-  const PagedCut K{std::max(1, PR_ROWS / (P.nq / P.nkv)), C::LG_UNIT, 1, INT32_MAX, PR_LEAST};
-  const PagedScratch S{static_cast<PagedCutItem *>(scratch), reinterpret_cast<float *>(static_cast<PagedCutItem *>(scratch) + PAGED_MAX_BLOCKS), PR_ROWS};
-  static_assert(PAGED_MAX_BLOCKS * (sizeof(PagedCutItem) + 2ull * PR_ROWS * (D + 2) * 4) <= DMTD_PAGED_ATTENTION_SCRATCH_BYTES, "scratch");
-  cudaError_t e = cudaFuncSetAttribute(paged_rows_kernel<T, KVT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  const int G = P.nq / P.nkv, blocks = std::min(2 * n_sms, ROWS_BLOCKS);
+  PagedCut K{PR_ROWS / G, C::LG_UNIT, 1, INT32_MAX, PR_LEAST};
+  cudaError_t e = cudaSuccess;
+  if constexpr (std::is_same<T, KVT>::value && !std::is_same<T, float>::value) {
+    const int min_new = (CHUNK_LEAST_ROWS + G - 1) / G;
+    if (max_new >= min_new) {
+      e = chunk_launch<T, D>(P, min_new, scratch, n_sms, stream);
+      K.max_new = min_new - 1;
+    }
+  }
+  const PagedScratch S = scratch_at(scratch, 0, ROWS_BLOCKS, PR_ROWS);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_rows_kernel<T, KVT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e == cudaSuccess) e = launch_pdl(paged_rows_kernel<T, KVT, D>, dim3(blocks), dim3(PR_THREADS), C::SMEM, stream, P, K, S);
   if (e == cudaSuccess) e = launch_pdl(paged_merge_kernel<T, KVT, D>, dim3(blocks, 1), dim3(PAGED_MERGE_WARPS * 32), 0, stream, P, S);
   return e;
 }
 
 template <int D>
-cudaError_t attention_launch(const PagedAttentionParams &P, int qt, int kv, void *scratch, int n_sms, cudaStream_t stream) {
-  if (qt == DMTD_BF16) return attention_launch_t<__nv_bfloat16, __nv_bfloat16, D>(P, scratch, n_sms, stream);
-  if (qt == DMTD_F16) return attention_launch_t<__half, __half, D>(P, scratch, n_sms, stream);
-  if (kv == DMTD_F32) return attention_launch_t<float, float, D>(P, scratch, n_sms, stream);
-  return kv == DMTD_BF16 ? attention_launch_t<float, __nv_bfloat16, D>(P, scratch, n_sms, stream)
-                         : attention_launch_t<float, __half, D>(P, scratch, n_sms, stream);
+cudaError_t attention_launch(const PagedAttentionParams &P, int qt, int kv, int max_new, void *scratch, int n_sms, cudaStream_t stream) {
+  if (qt == DMTD_BF16) return attention_launch_t<__nv_bfloat16, __nv_bfloat16, D>(P, max_new, scratch, n_sms, stream);
+  if (qt == DMTD_F16) return attention_launch_t<__half, __half, D>(P, max_new, scratch, n_sms, stream);
+  if (kv == DMTD_F32) return attention_launch_t<float, float, D>(P, max_new, scratch, n_sms, stream);
+  return kv == DMTD_BF16 ? attention_launch_t<float, __nv_bfloat16, D>(P, max_new, scratch, n_sms, stream)
+                         : attention_launch_t<float, __half, D>(P, max_new, scratch, n_sms, stream);
 }
 
 }  // namespace
@@ -195,8 +232,8 @@ dmtd_status dmtd_paged_attention(const void *q, int32_t q_dtype, int64_t q_strid
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int n_sms = sm_count();
   if (n_sms < 1) return call_failed(DMTD_ERR_CUDA, "paged_attention: device query failed");
-  return launched(D == 128 ? attention_launch<128>(P, q_dtype, cache->dtype, scratch, n_sms, stream)
-                           : attention_launch<64>(P, q_dtype, cache->dtype, scratch, n_sms, stream), "paged_attention");
+  return launched(D == 128 ? attention_launch<128>(P, q_dtype, cache->dtype, max_new ? max_new : n_rows, scratch, n_sms, stream)
+                           : attention_launch<64>(P, q_dtype, cache->dtype, max_new ? max_new : n_rows, scratch, n_sms, stream), "paged_attention");
 }
 
 }  // extern "C"

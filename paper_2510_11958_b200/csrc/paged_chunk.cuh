@@ -1,0 +1,518 @@
+// Attention of pieces of prompts over a paged cache on the 5th-generation tensor cores: 16-bit queries, cache of the same type.
+//
+// A block takes 256 query rows of one (request, kv head) - 256 / G positions x the G query heads - as two halves of 128, and
+// walks the keys they see in tiles of 128.  Per half and tile: S = Q K^T (M = 128 rows, N = 128 keys) into tensor memory,
+// softmax by a warpgroup (a thread owns a row: no shuffles), P back into tensor memory over S as the A operand of
+// O += P V.  The halves alternate: while one's softmax runs, the tensor cores work on the other's P V and next S.  P is handed
+// over in two parts, so that P V begins under the second half of the softmax.
+//
+// As in the row kernel a row's reference is raised only when a score lies more than 2^6 above it; then O is read
+// back and scaled.  S of a tile is committed behind P V of the tile before, so whoever has seen S may touch O.
+//
+// K and V tiles (rows of 64 values with the 128-byte swizzle, as K-major operand of S and as N-major operand of P V) come
+// through one ring, in turn, by 16-byte asynchronous copies whose pages are looked up a tile ahead.  One block per SM, persistent,
+// with an equal share of the line of work (paged_line.cuh): no tail, whatever the lengths are.
+//
+// Warps 0-3 and 4-7: softmax of the halves, queries, results; warp 8 issues the MMAs; warps 9 and 10 copy K and V; warp 11 lists the
+// pieces of the block's share (what the others would need 50 registers for).  Every wait is bounded: a block whose wait gives up leaves NaN in its rows.  Tensor memory is taken before the dependent grid is let in.
+#pragma once
+
+#include "paged_rows.cuh"
+
+namespace dmtd {
+
+constexpr int PC_M = 128, PC_ROWS = 2 * PC_M;                  // query rows of a half, of an item
+constexpr int PC_TK = 128, PC_LG_TK = 7;                       // keys of a tile: the unit of work
+constexpr int PC_THREADS = 384;
+constexpr int PC_LOADERS = 64;
+constexpr int PC_PIECES = 3;
+constexpr int PC_HALF = 128 * 128;                             // bytes of 64 dimensions of 128 rows
+constexpr float PC_ABOVE = 6.f;
+constexpr int PC_TMEM = 512;                                   // S (P over it) and O of both halves
+constexpr long long PC_WAIT_TICKS = 2000000000ll;              // about a second
+
+using ChunkShare = PagedShare<128, 64>;
+
+// A piece of a block's share as its warps go through it.
+struct ChunkPiece {
+  int b, row0, rows, kvh;            // request, first row of q, positions of the tile, kv head
+  int pos, keys;                     // position of the first row; keys that the last row sees
+  int u0, end[2];                    // key tiles [u0, end[h]) of half h
+  int began, ends, last;             // the item begins / ends in this piece; the share's last piece
+  int pieces;                        // of an item that goes on behind the share
+  __device__ __forceinline__ int last_tile() const { return max(end[0], end[1]); }
+};
+__device__ __forceinline__ ChunkPiece chunk_piece(const PagedPiece &p, long long line_end, const PagedCut &K, const ChunkShare &share, int G) {
+  ChunkPiece c;
+  c.b = p.r.b;
+  c.row0 = p.r.row0 + p.first(K);
+  c.rows = p.rows(K);
+  c.kvh = p.kvh;
+  c.pos = p.position(K);
+  c.keys = p.keys(K);
+  c.u0 = p.key_begin();
+  c.began = p.t0 == 0;
+  c.ends = p.t1 == p.per_item;
+  c.last = line_end >= share.end;
+  c.pieces = c.last && c.began && !c.ends ? share.holder(line_end - 1 + (p.per_item - p.t1)) - (int)blockIdx.x + 1 : 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    // keys that the half's last row sees
+    const int n = min(c.rows * G, (h + 1) * PC_M), keys = n > h * PC_M ? max(0, c.pos + (n - 1) / G + 1) : 0;
+    c.end[h] = max(c.u0, min(p.key_end(), (int)(((unsigned)keys + PC_TK - 1) >> PC_LG_TK)));
+  }
+  return c;
+}
+
+struct ChunkShared {
+  uint64_t q_full[2], s_full[2], o_full[2], p_full[2][2], full[8], empty[8], piece_full[PC_PIECES], piece_empty[PC_PIECES];
+  uint32_t tmem;
+  int gave_up;
+  ChunkPiece piece[PC_PIECES];
+  ChunkShare::Shared line;
+};
+
+template <int D>
+struct ChunkTypes {
+  static constexpr int PANELS = D / 64;                        // 128-byte wide columns of a tile
+  static constexpr int TILE = PANELS * PC_HALF;
+  static constexpr int Q = 0;
+  static constexpr int RING = 2 * TILE;
+  static constexpr int STAGES = D == 128 ? 5 : 8;
+  static constexpr int SMEM = RING + STAGES * TILE;
+  static_assert(SMEM + (int)sizeof(ChunkShared) <= 227 * 1024 - 16, "shared memory");
+};
+
+// byte offset of 16-byte part `part` of row `row` in a tile
+__device__ __forceinline__ uint32_t pc_part(int row, int part) {
+  return (uint32_t)((part >> 3) * PC_HALF + row * 128 + (((part & 7) ^ (row & 7)) << 4));
+}
+__device__ __forceinline__ uint64_t pc_desc(uint32_t addr, uint32_t lbo) { return umma_smem_desc(addr, lbo, 1024) | (2ull << 61); }
+
+// Bounded wait.  (No function calls in this kernel: the registers that setmaxnreg hands out are not for them.)
+__device__ __forceinline__ bool pc_wait(uint32_t bar, uint32_t parity, int *gave_up) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+#pragma unroll 1
+  for (int i = 1;; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (i % 64 == 0 && (*reinterpret_cast<volatile int *>(gave_up) || clock64() - t0 > PC_WAIT_TICKS)) {
+      *reinterpret_cast<volatile int *>(gave_up) = 1;
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid_constant__ PagedAttentionParams P, PagedCut K, PagedScratch S) {
+  using C = ChunkTypes<D>;
+  using Op = typename std::conditional<std::is_same<T, __half>::value, OpF16, OpBf16>::type;
+  constexpr float LIFT = std::is_same<T, __half>::value ? 8.f : 0.f;             // see the row kernel
+  extern __shared__ __align__(1024) unsigned char chunk_smem[];
+  __shared__ ChunkShared sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int G = P.nq / P.nkv, lg = P.pool.lg_page;
+  const uint32_t smem = smem_u32(chunk_smem);
+
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(smem_u32(&sh.q_full[h]), PC_M);
+      mbar_init(smem_u32(&sh.s_full[h]), 1);
+      mbar_init(smem_u32(&sh.o_full[h]), 1);
+      mbar_init(smem_u32(&sh.p_full[h][0]), PC_M);
+      mbar_init(smem_u32(&sh.p_full[h][1]), PC_M);
+    }
+    for (int i = 0; i < C::STAGES; ++i) {
+      mbar_init(smem_u32(&sh.full[i]), PC_LOADERS);
+      mbar_init(smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < PC_PIECES; ++i) {
+      mbar_init(smem_u32(&sh.piece_full[i]), 1);
+      mbar_init(smem_u32(&sh.piece_empty[i]), 11);             // a lane of every warp but the one that lists them
+    }
+    sh.gave_up = 0;
+    fence_mbar_init();
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(PC_TMEM) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  paged_enter();
+  const uint32_t tmem = sh.tmem;
+  ChunkShare share;
+  share.plan(P, K, sh.line, blockIdx.x, gridDim.x);
+  const bool work = share.begin < share.end;
+  if (!work && threadIdx.x == 0) S.items[blockIdx.x].pieces = 0;
+
+  if (work) {
+    // the next piece of the list; every warp but the last goes through all of them
+    int n_piece = 0;
+    auto take_piece = [&](ChunkPiece &c) {
+      const int i = n_piece % PC_PIECES;
+      const bool there = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.piece_full[i]), n_piece / PC_PIECES & 1, &sh.gave_up));
+      if (there) c = sh.piece[i];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.piece_empty[i]));
+      ++n_piece;
+      return there;
+    };
+    // registers: 256 x 216 + 128 x 72 = 384 x 168, what the block is launched with (the host checks it)
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 11) {
+      // ---- the list of pieces
+      if (lane == 0) {
+        PagedPiece p = share.find(P, K, sh.line, share.begin);
+        long long end = share.begin + (p.t1 - p.t0);
+        for (int n = 0;; ++n) {
+          const int i = n % PC_PIECES;
+          if (!pc_wait(smem_u32(&sh.piece_empty[i]), (n / PC_PIECES & 1) ^ 1, &sh.gave_up)) break;
+          sh.piece[i] = chunk_piece(p, end, K, share, G);
+          mbar_arrive(smem_u32(&sh.piece_full[i]));
+          if (!share.next(P, K, sh.line, p, end)) break;
+          end += p.t1 - p.t0;
+        }
+      }
+      __syncwarp();
+    } else if (warp >= 9) {
+      // ---- copies: K and V tiles in turn through the ring
+      const int lt = threadIdx.x - 9 * 32;
+      constexpr int PARTS = D / 8, STEP = PC_LOADERS / PARTS;  // rows that the threads take at a time
+      const int part = lt % PARTS, row_a = lt / PARTS;
+      const T *const base[2] = {reinterpret_cast<const T *>(P.pool.k), reinterpret_cast<const T *>(P.pool.v)};
+      int st = 0, ph = 0, pending = -1;                        // pending: the ring slot whose copies are under way
+      bool ok = true;
+      auto publish = [&]() {
+        if (pending >= 0) {
+          fence_proxy_async();
+          mbar_arrive(smem_u32(&sh.full[pending]));
+        }
+      };
+      ChunkPiece c;
+      while (ok && take_piece(c)) {
+        const int n_keys = c.keys, end = c.last_tile();
+        const int *table = P.batch.table + (size_t)c.b * P.batch.table_stride;
+        // lane i: the page of keys 4 i .. 4 i + 3 of the next tile (pages of less than four positions are looked up row by row)
+        auto look_up = [&](int tile) {
+          const int key = tile * PC_TK + lane * 4;
+          return key < n_keys ? table[key >> lg] : -1;
+        };
+        int ids = look_up(c.u0);
+        for (int i = c.u0; ok && i < end; ++i) {
+          const int ids_next = i + 1 < end ? look_up(i + 1) : -1;
+#pragma unroll 1
+          for (int kv = 0; kv < 2; ++kv) {
+            ok = pc_wait(smem_u32(&sh.empty[st]), ph ^ 1, &sh.gave_up);
+            if (!ok) break;
+            const uint32_t dst = smem + C::RING + st * C::TILE;
+            const T *src = base[kv] + c.kvh * P.pool.head_stride + part * 8;
+#pragma unroll 4
+            for (int r0 = 0; r0 < PC_TK; r0 += STEP) {         // (whole warps stay in the loop: the ids are asked of its lanes)
+              const int row = r0 + row_a, key = i * PC_TK + row;
+              int id;
+              if (lg >= 2) id = __shfl_sync(0xffffffffu, ids, (row >> 2) & 31);
+              else id = row < PC_TK && key < n_keys ? table[key >> lg] : -1;
+              const bool real = key < n_keys && id >= 0 && id < P.pool.n_pages;
+              if (row < PC_TK)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pc_part(row, part)),
+                             "l"(real ? src + id * P.pool.page_stride + (key & ((1 << lg) - 1)) * P.pool.row_stride : src), "r"(real ? 16 : 0)
+                             : "memory");
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            publish();
+            pending = st;
+            if (++st == C::STAGES) { st = 0; ph ^= 1; }
+          }
+          ids = ids_next;
+        }
+        if (c.last) break;
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      publish();
+    } else {
+      // ---- MMA issuer
+      constexpr uint32_t fmt = std::is_same<T, __half>::value ? 0u : 1u;
+      const uint32_t idesc_s = (1u << 4) | (fmt << 7) | (fmt << 10) | ((PC_TK >> 3) << 17) | ((PC_M >> 4) << 24);
+      const uint32_t idesc_o = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((D >> 3) << 17) | ((PC_M >> 4) << 24);
+      int st = 0, ph = 0, q_ph = 0, p_ph[2] = {0, 0};
+      bool ok = true;
+      auto all = [&](bool x) { return __all_sync(0xffffffffu, x); };
+      auto commit = [&](uint64_t &bar) {
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&bar)) : "memory");
+      };
+      auto scores = [&](int h, int slot) {
+        const uint32_t q = smem + C::Q + h * C::TILE, k = smem + C::RING + slot * C::TILE;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * PC_HALF + (kk & 3) * 32;
+          asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem + h * 128),
+                       "l"(pc_desc(q + off, 16)), "l"(pc_desc(k + off, 16)), "r"(idesc_s), "r"(kk > 0 ? 1u : 0u)
+                       : "memory");
+        }
+        commit(sh.s_full[h]);
+      };
+      auto values = [&](int h, int slot, int part, bool first) {           // 64 of the tile's keys
+        const uint32_t v = smem + C::RING + slot * C::TILE;
+#pragma unroll
+        for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
+          asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(tmem + 256 + h * 128),
+                       "r"(tmem + h * 128 + kk * 8), "l"(pc_desc(v + kk * 2048, PC_HALF)), "r"(idesc_o), "r"(first && kk == 0 ? 0u : 1u)
+                       : "memory");
+      };
+      ChunkPiece c;
+      while (ok && take_piece(c)) {
+        const int end = c.last_tile();
+        ok = all(pc_wait(smem_u32(&sh.q_full[0]), q_ph, &sh.gave_up) && pc_wait(smem_u32(&sh.q_full[1]), q_ph, &sh.gave_up));
+        q_ph ^= 1;
+        int k_slot = st;
+        auto advance = [&]() { if (++st == C::STAGES) { st = 0; ph ^= 1; } };
+        auto tile_there = [&]() {
+          ok = ok && all(pc_wait(smem_u32(&sh.full[st]), ph, &sh.gave_up));
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        };
+        if (ok && c.u0 < end) {
+          tile_there();
+          if (ok && elect_one()) {
+            if (c.u0 < c.end[0]) scores(0, st);
+            if (c.u0 < c.end[1]) scores(1, st);
+            commit(sh.empty[st]);
+          }
+          __syncwarp();
+          advance();
+        }
+        for (int i = c.u0; ok && i < end; ++i) {
+          tile_there();                                        // V of this tile
+          const int v_slot = st;
+          advance();
+          bool k_there = i + 1 >= end;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (i >= c.end[h]) continue;
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+              ok = ok && all(pc_wait(smem_u32(&sh.p_full[h][part]), p_ph[h], &sh.gave_up));
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              if (ok && elect_one()) values(h, v_slot, part, i == c.u0);
+              __syncwarp();
+            }
+            p_ph[h] ^= 1;
+            if (i + 1 < c.end[h]) {
+              if (!k_there) {                                  // K of the next tile
+                tile_there();
+                k_there = true;
+                k_slot = st;
+                advance();
+              }
+              if (ok && elect_one()) scores(h, k_slot);
+            } else {
+              if (ok && elect_one()) commit(sh.o_full[h]);
+            }
+            __syncwarp();
+          }
+          if (ok && elect_one()) {
+            commit(sh.empty[v_slot]);
+            if (i + 1 < end) commit(sh.empty[k_slot]);
+          }
+          __syncwarp();
+        }
+        if (c.last) break;
+      }
+    }
+    } else {
+      // ---- softmax: thread = query row = lane of tensor memory
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+      const int h = warp >> 2, row = threadIdx.x & 127, qi = h * PC_M + row;
+      const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+      const uint32_t t_s = tmem + h * 128 + lane_off, t_o = tmem + 256 + h * 128 + lane_off;
+      const float scale = 1.4426950408889634f * rsqrtf((float)D);
+      int s_ph = 0, o_ph = 0;
+      bool ok = true;
+      ChunkPiece c;
+      while (take_piece(c)) {
+        const int nQ = c.rows * G, n_keys = c.keys, end = h ? c.end[1] : c.end[0];
+        const int *table = P.batch.table + (size_t)c.b * P.batch.table_stride;
+        // ---- queries: this half's rows into shared memory (beyond the tile's rows zero)
+        bool holes;
+        {
+          constexpr int PARTS = D / 8, AT_ONCE = 128 / PARTS;
+          const int part = row % PARTS;
+          const T *q = reinterpret_cast<const T *>(P.q);
+          for (int r0 = 0; r0 < PC_M; r0 += AT_ONCE) {
+            const int r = r0 + row / PARTS, i = h * PC_M + r, p = i / G;
+            const bool real = i < nQ;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem + C::Q + h * C::TILE + pc_part(r, part)),
+                         "l"(real ? q + (c.row0 + p) * P.q_stride + (c.kvh * G + i - p * G) * D + part * 8 : q), "r"(real ? 16 : 0)
+                         : "memory");
+          }
+          // pages outside the pool: looked for once per piece
+          bool bad = false;
+          const int last = min(n_keys, c.last_tile() * PC_TK) - 1;
+          for (int pg = (c.u0 * PC_TK >> lg) + (int)threadIdx.x; last >= 0 && pg <= last >> lg; pg += 2 * PC_M) {
+            const int id = table[pg];
+            bad = bad || id < 0 || id >= P.pool.n_pages;
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          fence_proxy_async();
+          mbar_arrive(smem_u32(&sh.q_full[h]));
+          uint32_t r;
+          asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 256, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+                       : "=r"(r) : "r"((int)bad) : "memory");
+          holes = r != 0;
+        }
+
+        const int seen = qi < nQ ? c.pos + qi / G + 1 : 0;
+        float m = -INFINITY, l = 0.f;
+        for (int i = c.u0; ok && i < end; ++i) {
+          ok = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.s_full[h]), s_ph, &sh.gave_up));
+          s_ph ^= 1;
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          uint32_t s[128];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) tmem_ld32(t_s + 32 * j, *reinterpret_cast<uint32_t(*)[32]>(s + 32 * j));
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          const int lim = seen - i * PC_TK;                    // keys of the tile that this row sees
+          if (__any_sync(0xffffffffu, lim < PC_TK)) {
+#pragma unroll
+            for (int j = 0; j < 128; ++j) s[j] = j < lim ? s[j] : 0xff800000u;
+          }
+          if (holes) {
+#pragma unroll
+            for (int j0 = 0; j0 < 128; j0 += 32) {
+              const int key = i * PC_TK + j0 + lane, id = key < n_keys ? table[key >> lg] : -1;
+              const uint32_t good = __ballot_sync(0xffffffffu, id >= 0 && id < P.pool.n_pages);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) s[j0 + j] = (good >> j) & 1 ? s[j0 + j] : 0xff800000u;
+            }
+          }
+          float mx[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) mx[j] = fmaxf(__uint_as_float(s[j]), __uint_as_float(s[j + 4]));
+#pragma unroll
+          for (int j = 8; j < 128; j += 8) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[j + k]), __uint_as_float(s[j + 4 + k]));
+          }
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+          const bool grow = top > m + (PC_ABOVE + LIFT);
+          if (__any_sync(0xffffffffu, grow)) {
+            float alpha = 1.f;
+            if (grow) {
+              alpha = exp2_approx(m - (top - LIFT));
+              m = top - LIFT;
+              l *= alpha;
+            }
+            if (i > c.u0) {
+#pragma unroll 1
+              for (int c0 = 0; c0 < D; c0 += 16) {
+                uint32_t o[16];
+                tmem_ld16(t_o + c0, o);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                tmem_st16(t_o + c0, o);
+              }
+            }
+          }
+          const float ref = m > -INFINITY ? m : 0.f;
+          const uint64_t scale2 = f2_pack(scale, scale), ref2 = f2_pack(-ref, -ref);
+          uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+          for (int part = 0; part < 2; ++part) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              uint32_t p[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const int k = 64 * part + 32 * q + 2 * j;
+                float a, b;
+                f2_unpack(f2_fma(f2_pack(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), scale2, ref2), a, b);
+                a = exp2_approx(a);
+                b = exp2_approx(b);
+                sum[j & 1] = f2_add(sum[j & 1], f2_pack(a, b));
+                p[j] = Op::pack2(a, b);
+              }
+              tmem_st16(t_s + 32 * part + 16 * q, p);
+            }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            mbar_arrive(smem_u32(&sh.p_full[h][part]));
+          }
+          float l0, l1;
+          f2_unpack(f2_add(sum[0], sum[1]), l0, l1);
+          l += l0 + l1;
+        }
+
+        // ---- results
+        const bool any = end > c.u0, whole = c.began && c.ends;
+        if (any && ok) {
+          ok = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.o_full[h]), o_ph, &sh.gave_up));
+          o_ph ^= 1;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        }
+        const int p = qi / G, head = c.kvh * G + qi - p * G, place = paged_place(blockIdx.x, c.began);
+        const float inv = !ok ? NAN : l != 0.f ? 1.f / l : 0.f;
+        bool good = true;
+        if (!whole && qi < nQ) S.levels<D>(place)[qi] = make_float2(ok ? m : 0.f, ok ? l : NAN);
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 32) {
+          uint32_t o[32];
+          if (any) {
+            tmem_ld32(t_o + c0, o);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          }
+          if (qi < nQ) {
+            float f[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) f[j] = any && l != 0.f ? __uint_as_float(o[j]) : 0.f;
+            if (whole) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                f[j] *= inv;
+                good = good && isfinite(f[j]);
+              }
+              T *dst = reinterpret_cast<T *>(P.out) + ((size_t)(c.row0 + p) * P.nq + head) * D + c0;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) store_pack(dst + 8 * j, *reinterpret_cast<float(*)[8]>(f + 8 * j));
+            } else {
+              float *dst = S.sums<D>(place) + (size_t)qi * D + c0;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) store_pack(dst + 4 * j, *reinterpret_cast<float(*)[4]>(f + 4 * j));
+            }
+          }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        // rows that are not finite: see the row kernel
+        if (ok && c.rows > 1) {
+          uint32_t bad_rows = __ballot_sync(0xffffffffu, !good);
+          __syncwarp();
+          while (bad_rows) {
+            const int i = h * PC_M + (warp & 3) * 32 + __ffs(bad_rows) - 1, r = i / G;
+            bad_rows &= bad_rows - 1;
+            paged_attend_row_here<T, T, D>(P, c.b, c.row0 + r, c.pos + r + 1, c.kvh * G + i - r * G);
+          }
+        }
+        if (c.last) {
+          if (threadIdx.x == 0) S.items[blockIdx.x] = PagedCutItem{c.pieces, c.b, c.row0, c.rows, c.pos + 1, c.kvh, {0, 0}};
+          break;
+        }
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(PC_TMEM) : "memory");
+}
+
+}  // namespace dmtd

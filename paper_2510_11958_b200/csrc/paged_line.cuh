@@ -88,10 +88,10 @@ struct PagedPiece {
   __device__ __forceinline__ int position(const PagedCut &K) const { return r.c + i * K.tile; }
 };
 
-// THREADS threads of a block work out the line's length and their block's share.
-template <int THREADS>
+// The first THREADS threads of a block work out the line's length and their block's share.  KEPT: as many requests at most are
+// kept in shared memory; of larger batches they are read anew where they are needed.
+template <int THREADS, int KEPT>
 struct PagedShare {
-  static constexpr int KEPT = 2 * THREADS;               // requests kept in shared memory: others are read anew where they are needed
   long long total, begin, end;
   long long each, rest;              // a share's units: `each`, and `rest` of the shares have one more
   int n_blocks;

@@ -43,8 +43,9 @@ struct RowsPiece {
 };
 constexpr int PR_PIECES = 5;         // in a piece, its copies get as far as the third behind it, page ids to the fourth
 
+using RowsShare = PagedShare<PR_THREADS, 256>;
 struct RowsShared {
-  PagedShare<PR_THREADS>::Shared line;
+  RowsShare::Shared line;
   PagedPiece made;                   // the last piece made, by thread 0
   long long made_end;                // ... its end on the line
   RowsPiece piece[PR_PIECES];
@@ -309,7 +310,7 @@ struct RowsQueries {                 // what of the queries is in registers: all
 };
 
 // Thread 0: `p`, which ends at unit `end` of the line, as the warps need it.
-__device__ __forceinline__ void rows_describe(RowsPiece &d, const PagedPiece &p, long long end, const PagedCut &K, const PagedShare<PR_THREADS> &share) {
+__device__ __forceinline__ void rows_describe(RowsPiece &d, const PagedPiece &p, long long end, const PagedCut &K, const RowsShare &share) {
   const bool any = p.key_end() > p.key_begin();
   d.b = p.r.b;
   d.row0 = p.r.row0 + p.first(K);
@@ -335,7 +336,7 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
   const int G = P.nq / P.nkv, lg = P.pool.lg_page;
   const uint32_t g_inv = (65536 + G - 1) / G;                  // i / G == i * g_inv >> 16 for i < 16
   paged_enter();
-  PagedShare<PR_THREADS> share;
+  RowsShare share;
   share.plan(P, K, sh.line, blockIdx.x, gridDim.x);
   if (share.begin >= share.end) {
     if (threadIdx.x == 0) S.items[blockIdx.x].pieces = 0;

@@ -73,6 +73,35 @@ PagedScratch scratch_at(void *scratch, size_t offset, int blocks, int rows) {
   return PagedScratch{items, reinterpret_cast<float *>(items + blocks), rows};
 }
 
+// The pool as TMA sees it: [page][kv head][row][D], 64 dimensions of up to 128 rows of a page to a copy.
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+  static const EncodeTiled f = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) == cudaSuccess && found == cudaDriverEntryPointSuccess
+               ? reinterpret_cast<EncodeTiled>(p) : nullptr;
+  }();
+  return f;
+}
+ChunkMaps chunk_maps(const PagedPool &pool, int nkv, int D, bool f16) {
+  ChunkMaps m{};
+  if (pool.lg_page < 3 || !encode_tiled()) return m;
+  const cuuint64_t dims[4] = {(cuuint64_t)D, 1ull << pool.lg_page, (cuuint64_t)nkv, (cuuint64_t)pool.n_pages};
+  auto bytes = [&](long long stride) { return (cuuint64_t)(stride ? stride : D) * 2; };           // (of an axis of one: anything)
+  const cuuint64_t strides[3] = {bytes(pool.row_stride), bytes(pool.head_stride), bytes(pool.page_stride)};
+  const cuuint32_t box[4] = {64, (cuuint32_t)std::min(1 << pool.lg_page, PC_TK), 1, 1}, step[4] = {1, 1, 1, 1};
+  const void *base[2] = {pool.k, pool.v};
+  m.on = 1;
+  for (int i = 0; i < 2; ++i)
+    if (encode_tiled()(&m.map[i], f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base[i]), dims, strides, box,
+                       step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      m.on = 0;                                          // (strides that TMA cannot hold: 16-byte copies)
+  return m;
+}
+
 // Requests with at least this many query rows to a kv head go to the chunk kernel.
 constexpr int CHUNK_LEAST_ROWS = 65;
 
@@ -91,7 +120,8 @@ cudaError_t chunk_launch(const PagedAttentionParams &P, int min_new, void *scrat
   const PagedCut K{PC_ROWS / G, PC_LG_TK, min_new, INT32_MAX, 2};
   const PagedScratch S = scratch_at(scratch, scratch_part(ROWS_BLOCKS, PR_ROWS), CHUNK_BLOCKS, PC_ROWS);
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(blocks), dim3(PC_THREADS), C::SMEM, stream, P, K, S);
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(blocks), dim3(PC_THREADS), C::SMEM, stream, P,
+                                        chunk_maps(P.pool, P.nkv, D, std::is_same<T, __half>::value), K, S);
   if (e == cudaSuccess) e = launch_pdl(paged_merge_kernel<T, T, D>, dim3(blocks, PC_ROWS / PAGED_MERGE_WARPS), dim3(PAGED_MERGE_WARPS * 32), 0, stream, P, S);
   return e;
 }

@@ -10,12 +10,18 @@
 // back and scaled.  S of a tile is committed behind P V of the tile before, so whoever has seen S may touch O.
 //
 // K and V tiles (rows of 64 values with the 128-byte swizzle, as K-major operand of S and as N-major operand of P V) come
-// through one ring, in turn, by 16-byte asynchronous copies whose pages are looked up a tile ahead.  One block per SM, persistent,
-// with an equal share of the line of work (paged_line.cuh): no tail, whatever the lengths are.
+// through one ring, in turn, a TMA copy to a page and 64 dimensions; page ids are looked up a tile ahead.  Pages that are not there are
+// copied from behind the pool's end, which fills zeros; the page that holds the last key, whose rows behind it may hold anything,
+// comes by 16-byte copies that fill zeros (0 times a stale NaN would not be 0), and so does everything in pools whose pages have fewer than 8
+// positions (a swizzle atom).  (All copies 16 bytes wide, by two warps: 885 us for 2000 rows over 8000 keys, where the tensor cores
+// and the softmax take 250.)  One block per SM, persistent, with an equal share of the line of work (paged_line.cuh): no tail, whatever
+// the lengths are.
 //
-// Warps 0-3 and 4-7: softmax of the halves, queries, results; warp 8 issues the MMAs; warps 9 and 10 copy K and V; warp 11 lists the
+// Warps 0-3 and 4-7: softmax of the halves, queries, results; warp 8 issues the MMAs; warp 9 copies K, warp 10 V; warp 11 lists the
 // pieces of the block's share (what the others would need 50 registers for).  Every wait is bounded: a block whose wait gives up leaves NaN in its rows.  Tensor memory is taken before the dependent grid is let in.
 #pragma once
+
+#include <cuda.h>
 
 #include "paged_rows.cuh"
 
@@ -24,7 +30,6 @@ namespace dmtd {
 constexpr int PC_M = 128, PC_ROWS = 2 * PC_M;                  // query rows of a half, of an item
 constexpr int PC_TK = 128, PC_LG_TK = 7;                       // keys of a tile: the unit of work
 constexpr int PC_THREADS = 384;
-constexpr int PC_LOADERS = 64;
 constexpr int PC_PIECES = 3;
 constexpr int PC_HALF = 128 * 128;                             // bytes of 64 dimensions of 128 rows
 constexpr float PC_ABOVE = 6.f;
@@ -108,8 +113,21 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// The pool's K and V as arrays [page][kv head][row][D]; on: they can be described so, and pages hold a swizzle atom.
+struct ChunkMaps {
+  CUtensorMap map[2];
+  int on;
+};
+
+__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap *map, int c0, int row, int kvh, int page, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+               "l"(map), "r"(c0), "r"(row), "r"(kvh), "r"(page), "r"(bar)
+               : "memory");
+}
+
 template <typename T, int D>
-__global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid_constant__ PagedAttentionParams P, PagedCut K, PagedScratch S) {
+__global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid_constant__ PagedAttentionParams P,
+                                                                    const __grid_constant__ ChunkMaps M, PagedCut K, PagedScratch S) {
   using C = ChunkTypes<D>;
   using Op = typename std::conditional<std::is_same<T, __half>::value, OpF16, OpBf16>::type;
   constexpr float LIFT = std::is_same<T, __half>::value ? 8.f : 0.f;             // see the row kernel
@@ -129,7 +147,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       mbar_init(smem_u32(&sh.p_full[h][1]), PC_M);
     }
     for (int i = 0; i < C::STAGES; ++i) {
-      mbar_init(smem_u32(&sh.full[i]), PC_LOADERS);
+      mbar_init(smem_u32(&sh.full[i]), 2);                      // the bytes' announcement; the copies that are not TMA's
       mbar_init(smem_u32(&sh.empty[i]), 1);
     }
     for (int i = 0; i < PC_PIECES; ++i) {
@@ -184,19 +202,15 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       }
       __syncwarp();
     } else if (warp >= 9) {
-      // ---- copies: K and V tiles in turn through the ring
-      const int lt = threadIdx.x - 9 * 32;
-      constexpr int PARTS = D / 8, STEP = PC_LOADERS / PARTS;  // rows that the threads take at a time
-      const int part = lt % PARTS, row_a = lt / PARTS;
-      const T *const base[2] = {reinterpret_cast<const T *>(P.pool.k), reinterpret_cast<const T *>(P.pool.v)};
-      int st = 0, ph = 0, pending = -1;                        // pending: the ring slot whose copies are under way
+      // ---- copies: warp 9 the K tiles, warp 10 the V tiles, which take turns in the ring
+      const int kv = warp - 9;
+      constexpr int PARTS = D / 8;
+      const T *const base = reinterpret_cast<const T *>(kv ? P.pool.v : P.pool.k);
+      const CUtensorMap *const map = &M.map[kv];
+      const int rows_here = min(1 << lg, PC_TK);               // of a tile, in one page
+      const int n_pages = PC_TK / rows_here;                   // pages of a tile
+      int n = kv;                                              // place in the order of tiles
       bool ok = true;
-      auto publish = [&]() {
-        if (pending >= 0) {
-          fence_proxy_async();
-          mbar_arrive(smem_u32(&sh.full[pending]));
-        }
-      };
       ChunkPiece c;
       while (ok && take_piece(c)) {
         const int n_keys = c.keys, end = c.last_tile();
@@ -207,38 +221,54 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
           return key < n_keys ? table[key >> lg] : -1;
         };
         int ids = look_up(c.u0);
-        for (int i = c.u0; ok && i < end; ++i) {
+        for (int i = c.u0; i < end; ++i, n += 2) {
           const int ids_next = i + 1 < end ? look_up(i + 1) : -1;
-#pragma unroll 1
-          for (int kv = 0; kv < 2; ++kv) {
-            ok = pc_wait(smem_u32(&sh.empty[st]), ph ^ 1, &sh.gave_up);
-            if (!ok) break;
-            const uint32_t dst = smem + C::RING + st * C::TILE;
-            const T *src = base[kv] + c.kvh * P.pool.head_stride + part * 8;
-#pragma unroll 4
-            for (int r0 = 0; r0 < PC_TK; r0 += STEP) {         // (whole warps stay in the loop: the ids are asked of its lanes)
-              const int row = r0 + row_a, key = i * PC_TK + row;
-              int id;
-              if (lg >= 2) id = __shfl_sync(0xffffffffu, ids, (row >> 2) & 31);
-              else id = row < PC_TK && key < n_keys ? table[key >> lg] : -1;
-              const bool real = key < n_keys && id >= 0 && id < P.pool.n_pages;
-              if (row < PC_TK)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pc_part(row, part)),
-                             "l"(real ? src + id * P.pool.page_stride + (key & ((1 << lg) - 1)) * P.pool.row_stride : src), "r"(real ? 16 : 0)
-                             : "memory");
+          const int st = n % C::STAGES, left = n_keys - i * PC_TK;
+          ok = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.empty[st]), (n / C::STAGES & 1) ^ 1, &sh.gave_up));
+          if (!ok) break;
+          const uint32_t dst = smem + C::RING + st * C::TILE, bar = smem_u32(&sh.full[st]);
+          // rows [0, whole) by TMA, the page that the last key shares with rows behind it and nothing else by the lanes
+          const int whole = !M.on ? 0 : left >= PC_TK ? PC_TK : left / rows_here * rows_here;
+          const int rest = !M.on ? PC_TK : whole < left ? min(PC_TK, whole + rows_here) : whole;          // rows [whole, rest) by the lanes
+          if (lane == 0) mbar_expect_tx(bar, (PC_TK - (rest - whole)) * D * (int)sizeof(T));
+          __syncwarp();
+          if (M.on) {
+            const int panel = lane / n_pages, pg = lane % n_pages, row = pg * rows_here;
+            int id = __shfl_sync(0xffffffffu, ids, row >> 2);
+            if (panel < C::PANELS && (row < whole || row >= rest)) {
+              if (row >= whole || id < 0 || id >= P.pool.n_pages) id = P.pool.n_pages;          // behind the end: zeros
+              tma_page(dst + panel * PC_HALF + row * 128, map, panel * 64, i * PC_TK & ((1 << lg) - 1), c.kvh, id, bar);
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
-            publish();
-            pending = st;
-            if (++st == C::STAGES) { st = 0; ph ^= 1; }
           }
+          if (rest > whole) {
+            const T *src = base + c.kvh * P.pool.head_stride;
+#pragma unroll 4
+            for (int j = lane; j < (rest - whole) * PARTS; j += 32) {
+              const int row = whole + j / PARTS, part = j % PARTS, key = i * PC_TK + row;
+              const int id = key < n_keys ? table[key >> lg] : -1;
+              const bool real = id >= 0 && id < P.pool.n_pages;
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pc_part(row, part)),
+                           "l"(real ? src + id * P.pool.page_stride + (key & ((1 << lg) - 1)) * P.pool.row_stride + part * 8 : src), "r"(real ? 16 : 0)
+                           : "memory");
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_proxy_async();
+            __syncwarp();
+          }
+          if (lane == 0) mbar_arrive(bar);
           ids = ids_next;
         }
         if (c.last) break;
       }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      publish();
+      // leave no copy in flight: the last tiles of a block that gave up get a bounded wait
+      if (!ok && lane == 0) {
+        for (int k = max(kv, n - 2 * C::STAGES); k < n; k += 2) {
+          const long long t0 = clock64();
+          while (!mbar_try_wait(smem_u32(&sh.full[k % C::STAGES]), k / C::STAGES & 1))
+            if (clock64() - t0 > PC_WAIT_TICKS) break;
+        }
+      }
+      __syncwarp();
     } else {
       // ---- MMA issuer
       constexpr uint32_t fmt = std::is_same<T, __half>::value ? 0u : 1u;

@@ -106,10 +106,9 @@ ChunkMaps chunk_maps(const PagedPool &pool, int nkv, int D, bool f16) {
 constexpr int CHUNK_LEAST_ROWS = 65;
 
 template <typename T, int D>
-cudaError_t chunk_launch(const PagedAttentionParams &P, int min_new, void *scratch, int n_sms, cudaStream_t stream) {
+cudaError_t chunk_launch(const PagedAttentionParams &P, int min_new, const PagedScratch &S, int blocks, cudaStream_t stream) {
   using C = ChunkTypes<D>;
   const auto kernel = paged_chunk_kernel<T, D>;
-  const int G = P.nq / P.nkv, blocks = std::min(n_sms, CHUNK_BLOCKS);
   // the warpgroups' shares are taken out of the registers that the block was launched with: with fewer they would wait for ever
   static const bool enough = [&] {
     cudaFuncAttributes a;
@@ -117,12 +116,10 @@ cudaError_t chunk_launch(const PagedAttentionParams &P, int min_new, void *scrat
   }();
   if (!enough) return cudaErrorInvalidConfiguration;
   cudaError_t e;
-  const PagedCut K{PC_ROWS / G, PC_LG_TK, min_new, INT32_MAX, 2};
-  const PagedScratch S = scratch_at(scratch, scratch_part(ROWS_BLOCKS, PR_ROWS), CHUNK_BLOCKS, PC_ROWS);
+  const PagedCut K{PC_ROWS / (P.nq / P.nkv), PC_LG_TK, min_new, INT32_MAX, 2};
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(blocks), dim3(PC_THREADS), C::SMEM, stream, P,
                                         chunk_maps(P.pool, P.nkv, D, std::is_same<T, __half>::value), K, S);
-  if (e == cudaSuccess) e = launch_pdl(paged_merge_kernel<T, T, D>, dim3(blocks, PC_ROWS / PAGED_MERGE_WARPS), dim3(PAGED_MERGE_WARPS * 32), 0, stream, P, S);
   return e;
 }
 
@@ -131,18 +128,24 @@ cudaError_t attention_launch_t(const PagedAttentionParams &P, int max_new, void 
   using C = RowsTypes<T, KVT, D>;
   const int G = P.nq / P.nkv, blocks = std::min(2 * n_sms, ROWS_BLOCKS);
   PagedCut K{PR_ROWS / G, C::LG_UNIT, 1, INT32_MAX, PR_LEAST};
+  const PagedScratch S = scratch_at(scratch, 0, ROWS_BLOCKS, PR_ROWS);
+  const PagedScratch S_chunk = scratch_at(scratch, scratch_part(ROWS_BLOCKS, PR_ROWS), CHUNK_BLOCKS, PC_ROWS);
+  int chunk_blocks = 0;
   cudaError_t e = cudaSuccess;
   if constexpr (std::is_same<T, KVT>::value && !std::is_same<T, float>::value) {
     const int min_new = (CHUNK_LEAST_ROWS + G - 1) / G;
     if (max_new >= min_new) {
-      e = chunk_launch<T, D>(P, min_new, scratch, n_sms, stream);
+      chunk_blocks = std::min(n_sms, CHUNK_BLOCKS);
+      e = chunk_launch<T, D>(P, min_new, S_chunk, chunk_blocks, stream);
       K.max_new = min_new - 1;
     }
   }
-  const PagedScratch S = scratch_at(scratch, 0, ROWS_BLOCKS, PR_ROWS);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_rows_kernel<T, KVT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-  if (e == cudaSuccess) e = launch_pdl(paged_rows_kernel<T, KVT, D>, dim3(blocks), dim3(PR_THREADS), C::SMEM, stream, P, K, S);
-  if (e == cudaSuccess) e = launch_pdl(paged_merge_kernel<T, KVT, D>, dim3(blocks, 1), dim3(PAGED_MERGE_WARPS * 32), 0, stream, P, S);
+  if (e == cudaSuccess)
+    e = launch_pdl(paged_rows_kernel<T, KVT, D>, dim3(blocks), dim3(PR_THREADS), C::SMEM, stream, P, K, S, chunk_blocks > 0);
+  if (e == cudaSuccess)
+    e = launch_pdl(paged_merge_kernel<T, KVT, D>, dim3(blocks + chunk_blocks * (PC_ROWS / PAGED_MERGE_ROWS)), dim3(PAGED_MERGE_WARPS * 32), 0, stream, P, S,
+                   blocks, S_chunk);
   return e;
 }
 

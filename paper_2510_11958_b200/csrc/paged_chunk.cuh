@@ -164,7 +164,10 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  paged_enter();
+  // in this order: the row kernel behind does not wait for what is in front of this one (and no grid may hold tensor memory's
+  // columns off this block while it waits)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem = sh.tmem;
   ChunkShare share;
   share.plan(P, K, sh.line, blockIdx.x, gridDim.x);

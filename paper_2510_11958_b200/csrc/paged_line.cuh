@@ -222,64 +222,93 @@ struct PagedScratch {
 // A block's place for the piece of an item that began in an earlier block / that goes on in a later one.
 __device__ __forceinline__ int paged_place(int block, bool began_here) { return 2 * block + (began_here ? 1 : 0); }
 
-// grid (blocks of the attention's launch, row groups): block (j, y) joins rows of the item that is cut at the end of block
-// j's share.  Levels are powers of two.  A warp takes a query row at a time: its lanes fetch the pieces' levels side by
-// side, and all lanes the pieces' sums, which do not wait for the levels.
-constexpr int PAGED_MERGE_WARPS = 16;
-template <typename T, typename KVT, int D>
-__global__ void __launch_bounds__(PAGED_MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ PagedAttentionParams P, PagedScratch S) {
-  constexpr int E = D / 32, DEEP = 8;
-  paged_enter();
-  const PagedCutItem c = S.items[blockIdx.x];
-  if (c.pieces == 0) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = P.nq / P.nkv;
-  for (int qi = blockIdx.y * PAGED_MERGE_WARPS + warp; qi < c.rows * G; qi += gridDim.y * PAGED_MERGE_WARPS) {
-    float m = -INFINITY, l = 0.f, o[E];
+// Joins query rows q0 .. q0 + AT_ONCE - 1 of the item that is cut at the end of `block`'s share, by one warp.  Levels are powers of
+// two.  The lanes fetch the pieces' levels side by side, and all lanes the pieces' sums, which do not wait for the levels.
+template <typename T, typename KVT, int D, int AT_ONCE, int DEEP>
+__device__ __forceinline__ void paged_join(const PagedAttentionParams &P, const PagedScratch &S, const PagedCutItem &c, int block, int q0) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31, G = P.nq / P.nkv, nQ = c.rows * G;
+  float m[AT_ONCE], l[AT_ONCE], o[AT_ONCE][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int s0 = 0; s0 < c.pieces; s0 += 32) {
-      const int n = min(32, c.pieces - s0);
-      auto place = [&](int s) { return paged_place(blockIdx.x + s0 + s, s0 + s == 0); };
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (lane < n) ml = S.levels<D>(place(lane))[qi];
-      float v[DEEP][E];
-      auto load = [&](int first) {
+  for (int k = 0; k < AT_ONCE; ++k) {
+    m[k] = -INFINITY;
+    l[k] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[k][e] = 0.f;
+  }
+  for (int s0 = 0; s0 < c.pieces; s0 += 32) {
+    const int n = min(32, c.pieces - s0);
+    auto place = [&](int s) { return paged_place(block + s0 + s, s0 + s == 0); };
+    float2 ml[AT_ONCE];
+    float v[AT_ONCE][DEEP][E], w[AT_ONCE];
+    auto load = [&](int first) {
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) {
 #pragma unroll
         for (int s = 0; s < DEEP; ++s)
-          if (first + s < n) load_pack(S.sums<D>(place(first + s)) + (size_t)qi * D + lane * E, v[s]);
-      };
-      load(0);
-      const float top = fmaxf(m, warp_max(ml.x));
-      const float old = m > -INFINITY ? exp2f(m - top) : 0.f;
-      const float w = ml.x > -INFINITY ? exp2f(ml.x - top) : 0.f;
-      l = l * old + warp_sum(ml.y * w);
+          if (first + s < n && q0 + k < nQ) load_pack(S.sums<D>(place(first + s)) + (size_t)(q0 + k) * D + lane * E, v[k][s]);
+      }
+    };
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] *= old;
-      for (int first = 0; first < n; first += DEEP) {
-        if (first > 0) load(first);
+    for (int k = 0; k < AT_ONCE; ++k) ml[k] = lane < n && q0 + k < nQ ? S.levels<D>(place(lane))[q0 + k] : make_float2(-INFINITY, 0.f);
+    load(0);
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const float top = fmaxf(m[k], warp_max(ml[k].x));
+      const float old = m[k] > -INFINITY ? exp2f(m[k] - top) : 0.f;
+      w[k] = ml[k].x > -INFINITY ? exp2f(ml[k].x - top) : 0.f;
+      l[k] = l[k] * old + warp_sum(ml[k].y * w[k]);
+      m[k] = top;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[k][e] *= old;
+    }
+    for (int first = 0; first < n; first += DEEP) {
+      if (first > 0) load(first);
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) {
 #pragma unroll
         for (int s = 0; s < DEEP; ++s) {
-          const float ws = __shfl_sync(0xffffffffu, w, (first + s) & 31);
-          if (first + s < n && ws != 0.f) {
+          const float ws = __shfl_sync(0xffffffffu, w[k], (first + s) & 31);
+          if (first + s < n && q0 + k < nQ && ws != 0.f) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = fmaf(ws, v[s][e], o[e]);
+            for (int e = 0; e < E; ++e) o[k][e] = fmaf(ws, v[k][s][e], o[k][e]);
           }
         }
       }
-      m = top;
     }
+  }
+#pragma unroll
+  for (int k = 0; k < AT_ONCE; ++k) {
+    if (q0 + k >= nQ) break;
     bool good = true;
+    const float inv = l[k] != 0.f ? 1.f / l[k] : 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      o[e] = l != 0.f ? o[e] / l : 0.f;
-      good = good && isfinite(o[e]);
+      o[k][e] = l[k] != 0.f ? o[k][e] * inv : 0.f;
+      good = good && isfinite(o[k][e]);
     }
-    const int r = qi / G, row = c.row0 + r, head = c.kvh * G + qi % G;
-    if (c.rows > 1 && !__all_sync(0xffffffffu, good)) {
-      paged_attend_row<T, KVT, D>(P, c.b, row, c.first_seen + r, head);
-    } else {
-      store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o);
-    }
+    const int r = (q0 + k) / G, row = c.row0 + r, head = c.kvh * G + q0 + k - r * G;
+    if (c.rows > 1 && !__all_sync(0xffffffffu, good)) paged_attend_row<T, KVT, D>(P, c.b, row, c.first_seen + r, head);
+    else store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o[k]);
+  }
+}
+
+// Joins what was cut: a block to each of the row kernel's `blocks` shares, a warp to a row; then, if the chunk kernel ran
+// too, 256 / PAGED_MERGE_ROWS blocks to each of its shares, a warp to four rows (items of it are cut into two or three as a rule).
+constexpr int PAGED_MERGE_WARPS = 16, PAGED_MERGE_ROWS = PAGED_MERGE_WARPS * 4;
+template <typename T, typename KVT, int D>
+__global__ void __launch_bounds__(PAGED_MERGE_WARPS * 32, 2) paged_merge_kernel(const __grid_constant__ PagedAttentionParams P, PagedScratch S,
+                                                                                 int blocks, PagedScratch S_chunk) {
+  paged_enter();
+  const int warp = threadIdx.x >> 5;
+  if ((int)blockIdx.x < blocks) {
+    const PagedCutItem c = S.items[blockIdx.x];
+    if (c.pieces && warp < c.rows * (P.nq / P.nkv)) paged_join<T, KVT, D, 1, 8>(P, S, c, blockIdx.x, warp);
+  } else {
+    const int per = S_chunk.rows / PAGED_MERGE_ROWS, block = (blockIdx.x - blocks) / per, part = (blockIdx.x - blocks) % per;
+    const PagedCutItem c = S_chunk.items[block];
+    const int q0 = (part * PAGED_MERGE_WARPS + warp) * 4;
+    if (c.pieces && q0 < c.rows * (P.nq / P.nkv)) paged_join<T, KVT, D, 4, 2>(P, S_chunk, c, block, q0);
   }
 }
 

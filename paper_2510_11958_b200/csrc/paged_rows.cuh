@@ -327,7 +327,8 @@ __device__ __forceinline__ void rows_describe(RowsPiece &d, const PagedPiece &p,
 }
 
 template <typename T, typename KVT, int D>
-__global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_constant__ PagedAttentionParams P, PagedCut K, PagedScratch S) {
+__global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_constant__ PagedAttentionParams P, PagedCut K, PagedScratch S,
+                                                                    int behind_chunk) {
   using C = RowsTypes<T, KVT, D>;
   using Op = typename std::conditional<std::is_same<KVT, __half>::value, OpF16, OpBf16>::type;
   extern __shared__ __align__(128) unsigned char sc[];
@@ -335,11 +336,16 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int G = P.nq / P.nkv, lg = P.pool.lg_page;
   const uint32_t g_inv = (65536 + G - 1) / G;                  // i / G == i * g_inv >> 16 for i < 16
-  paged_enter();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // Behind the chunk kernel this one was let in by blocks that had waited for everything in front of them, and it reads nothing that
+  // they write: it waits at its end, for the grids behind it.
+  auto wait = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
+  if (!behind_chunk) wait();
   RowsShare share;
   share.plan(P, K, sh.line, blockIdx.x, gridDim.x);
   if (share.begin >= share.end) {
     if (threadIdx.x == 0) S.items[blockIdx.x].pieces = 0;
+    if (behind_chunk) wait();
     return;
   }
   // thread 0 keeps the list of pieces five ahead, so that what a piece looks at was made before a barrier
@@ -614,6 +620,7 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
     }
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
+  if (behind_chunk) wait();
 }
 
 }  // namespace dmtd

@@ -109,15 +109,8 @@ template <typename T, int D>
 cudaError_t chunk_launch(const PagedAttentionParams &P, int min_new, const PagedScratch &S, int blocks, cudaStream_t stream) {
   using C = ChunkTypes<D>;
   const auto kernel = paged_chunk_kernel<T, D>;
-  // the warpgroups' shares are taken out of the registers that the block was launched with: with fewer they would wait for ever
-  static const bool enough = [&] {
-    cudaFuncAttributes a;
-    return cudaFuncGetAttributes(&a, kernel) == cudaSuccess && a.numRegs >= 168;
-  }();
-  if (!enough) return cudaErrorInvalidConfiguration;
-  cudaError_t e;
   const PagedCut K{PC_ROWS / (P.nq / P.nkv), PC_LG_TK, min_new, INT32_MAX, 2};
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(blocks), dim3(PC_THREADS), C::SMEM, stream, P,
                                         chunk_maps(P.pool, P.nkv, D, std::is_same<T, __half>::value), K, S);
   return e;
@@ -144,7 +137,7 @@ cudaError_t attention_launch_t(const PagedAttentionParams &P, int max_new, void 
   if (e == cudaSuccess)
     e = launch_pdl(paged_rows_kernel<T, KVT, D>, dim3(blocks), dim3(PR_THREADS), C::SMEM, stream, P, K, S, chunk_blocks > 0);
   if (e == cudaSuccess)
-    e = launch_pdl(paged_merge_kernel<T, KVT, D>, dim3(blocks + chunk_blocks * (PC_ROWS / PAGED_MERGE_ROWS)), dim3(PAGED_MERGE_WARPS * 32), 0, stream, P, S,
+    e = launch_pdl(paged_merge_kernel<T, KVT, D>, dim3(blocks + chunk_blocks * paged_merge_per_chunk<D>(PC_ROWS)), dim3(PAGED_MERGE_WARPS * 32), 0, stream, P, S,
                    blocks, S_chunk);
   return e;
 }

@@ -1,13 +1,15 @@
 // Attention of pieces of prompts over a paged cache on the 5th-generation tensor cores: 16-bit queries, cache of the same type.
 //
 // A block takes 256 query rows of one (request, kv head) - 256 / G positions x the G query heads - as two halves of 128, and
-// walks the keys they see in tiles of 128.  Per half and tile: S = Q K^T (M = 128 rows, N = 128 keys) into tensor memory,
-// softmax by a warpgroup (a thread owns a row: no shuffles), P back into tensor memory over S as the A operand of
-// O += P V.  The halves alternate: while one's softmax runs, the tensor cores work on the other's P V and next S.  P is handed
-// over in two parts, so that P V begins under the second half of the softmax.
+// walks the keys they see in steps of 64.  Per half and step: S = Q K^T (M = 128 rows, N = 64 keys) into one of two places in
+// tensor memory, softmax by a warpgroup (a thread owns a row: no shuffles), P back into tensor memory over S as the A operand
+// of O += P V.  While a half's softmax runs, its next S is there already and the tensor cores work on the other half.  (Steps
+// of 128 keys have room for one S to a half: softmax and tensor cores took turns, 4125 cycles for 128 keys and 256 rows; 2048 is the tensor
+// cores' least, 2560 with N = 64, which reads Q twice as often.)  Each half has an issuing warp of its own: an MMA takes a warp some 70
+// cycles to issue, and one warp for both halves was the bound of it all (6130 cycles).
 //
 // As in the row kernel a row's reference is raised only when a score lies more than 2^6 above it; then O is read
-// back and scaled.  S of a tile is committed behind P V of the tile before, so whoever has seen S may touch O.
+// back and scaled.
 //
 // K and V tiles (rows of 64 values with the 128-byte swizzle, as K-major operand of S and as N-major operand of P V) come
 // through one ring, in turn, a TMA copy to a page and 64 dimensions; page ids are looked up a tile ahead.  Pages that are not there are
@@ -17,8 +19,8 @@
 // and the softmax take 250.)  One block per SM, persistent, with an equal share of the line of work (paged_line.cuh): no tail, whatever
 // the lengths are.
 //
-// Warps 0-3 and 4-7: softmax of the halves, queries, results; warp 8 issues the MMAs; warp 9 copies K, warp 10 V; warp 11 lists the
-// pieces of the block's share (what the others would need 50 registers for).  Every wait is bounded: a block whose wait gives up leaves NaN in its rows.  Tensor memory is taken before the dependent grid is let in.
+// Warps 0-3 and 4-7: softmax of the halves, queries, results; warps 8 and 9 issue their MMAs; warp 10 copies K and V; warp 11 lists the
+// pieces of the block's share (what the others would need 50 registers for).  Every wait is bounded: a block whose wait gives up leaves NaN in the rows at hand and the rest unwritten.  Tensor memory is taken before the dependent grid is let in.
 #pragma once
 
 #include <cuda.h>
@@ -28,12 +30,13 @@
 namespace dmtd {
 
 constexpr int PC_M = 128, PC_ROWS = 2 * PC_M;                  // query rows of a half, of an item
-constexpr int PC_TK = 128, PC_LG_TK = 7;                       // keys of a tile: the unit of work
+constexpr int PC_TK = 128, PC_LG_TK = 7;                       // keys of a tile of the ring: the unit of work
+constexpr int PC_STEP = 64;                                    // keys of a step
 constexpr int PC_THREADS = 384;
 constexpr int PC_PIECES = 3;
 constexpr int PC_HALF = 128 * 128;                             // bytes of 64 dimensions of 128 rows
 constexpr float PC_ABOVE = 6.f;
-constexpr int PC_TMEM = 512;                                   // S (P over it) and O of both halves
+constexpr int PC_TMEM = 512;                                   // two S (P over them) and O of both halves
 constexpr long long PC_WAIT_TICKS = 2000000000ll;              // about a second
 
 using ChunkShare = PagedShare<128, 64>;
@@ -42,10 +45,12 @@ using ChunkShare = PagedShare<128, 64>;
 struct ChunkPiece {
   int b, row0, rows, kvh;            // request, first row of q, positions of the tile, kv head
   int pos, keys;                     // position of the first row; keys that the last row sees
-  int u0, end[2];                    // key tiles [u0, end[h]) of half h
+  int u0, end[2];                    // first key tile; half h takes steps [2 u0, end[h])
   int began, ends, last;             // the item begins / ends in this piece; the share's last piece
   int pieces;                        // of an item that goes on behind the share
-  __device__ __forceinline__ int last_tile() const { return max(end[0], end[1]); }
+  int holes;                         // some page of the piece is outside the pool
+  __device__ __forceinline__ int last_step() const { return max(end[0], end[1]); }
+  __device__ __forceinline__ int last_tile() const { return (last_step() + 1) >> 1; }
 };
 __device__ __forceinline__ ChunkPiece chunk_piece(const PagedPiece &p, long long line_end, const PagedCut &K, const ChunkShare &share, int G) {
   ChunkPiece c;
@@ -60,17 +65,18 @@ __device__ __forceinline__ ChunkPiece chunk_piece(const PagedPiece &p, long long
   c.ends = p.t1 == p.per_item;
   c.last = line_end >= share.end;
   c.pieces = c.last && c.began && !c.ends ? share.holder(line_end - 1 + (p.per_item - p.t1)) - (int)blockIdx.x + 1 : 0;
+  c.holes = 0;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     // keys that the half's last row sees
     const int n = min(c.rows * G, (h + 1) * PC_M), keys = n > h * PC_M ? max(0, c.pos + (n - 1) / G + 1) : 0;
-    c.end[h] = max(c.u0, min(p.key_end(), (int)(((unsigned)keys + PC_TK - 1) >> PC_LG_TK)));
+    c.end[h] = max(2 * c.u0, min(2 * p.key_end(), (int)(((unsigned)keys + PC_STEP - 1) / PC_STEP)));
   }
   return c;
 }
 
 struct ChunkShared {
-  uint64_t q_full[2], s_full[2], o_full[2], p_full[2][2], full[8], empty[8], piece_full[PC_PIECES], piece_empty[PC_PIECES];
+  uint64_t q_full[2], s_full[2][2], p_full[2][2], o_done[2], o_full[2], full[8], empty[8], piece_full[PC_PIECES], piece_empty[PC_PIECES];
   uint32_t tmem;
   int gave_up;
   ChunkPiece piece[PC_PIECES];
@@ -94,7 +100,7 @@ __device__ __forceinline__ uint32_t pc_part(int row, int part) {
 }
 __device__ __forceinline__ uint64_t pc_desc(uint32_t addr, uint32_t lbo) { return umma_smem_desc(addr, lbo, 1024) | (2ull << 61); }
 
-// Bounded wait.  (No function calls in this kernel: the registers that setmaxnreg hands out are not for them.)
+// Bounded wait.
 __device__ __forceinline__ bool pc_wait(uint32_t bar, uint32_t parity, int *gave_up) {
   if (mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
@@ -141,14 +147,16 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       mbar_init(smem_u32(&sh.q_full[h]), PC_M);
-      mbar_init(smem_u32(&sh.s_full[h]), 1);
-      mbar_init(smem_u32(&sh.o_full[h]), 1);
-      mbar_init(smem_u32(&sh.p_full[h][0]), PC_M);
-      mbar_init(smem_u32(&sh.p_full[h][1]), PC_M);
+      mbar_init(smem_u32(&sh.o_done[h]), 1);                   // P V of a step
+      mbar_init(smem_u32(&sh.o_full[h]), 1);                   // ... of a piece's last step (two steps may be under way then: a phase of its own)
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(smem_u32(&sh.s_full[h][i]), 1);
+        mbar_init(smem_u32(&sh.p_full[h][i]), PC_M);
+      }
     }
     for (int i = 0; i < C::STAGES; ++i) {
       mbar_init(smem_u32(&sh.full[i]), 2);                      // the bytes' announcement; the copies that are not TMA's
-      mbar_init(smem_u32(&sh.empty[i]), 1);
+      mbar_init(smem_u32(&sh.empty[i]), 2);                     // both halves
     }
     for (int i = 0; i < PC_PIECES; ++i) {
       mbar_init(smem_u32(&sh.piece_full[i]), 1);
@@ -172,7 +180,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
   ChunkShare share;
   share.plan(P, K, sh.line, blockIdx.x, gridDim.x);
   const bool work = share.begin < share.end;
-  if (!work && threadIdx.x == 0) S.items[blockIdx.x].pieces = 0;
+  if (threadIdx.x == 0) S.items[blockIdx.x].pieces = 0;       // (written anew with the last piece)
 
   if (work) {
     // the next piece of the list; every warp but the last goes through all of them
@@ -186,33 +194,38 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       ++n_piece;
       return there;
     };
-    // registers: 256 x 216 + 128 x 72 = 384 x 168, what the block is launched with (the host checks it)
-    if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 11) {
       // ---- the list of pieces
-      if (lane == 0) {
-        PagedPiece p = share.find(P, K, sh.line, share.begin);
-        long long end = share.begin + (p.t1 - p.t0);
-        for (int n = 0;; ++n) {
-          const int i = n % PC_PIECES;
-          if (!pc_wait(smem_u32(&sh.piece_empty[i]), (n / PC_PIECES & 1) ^ 1, &sh.gave_up)) break;
-          sh.piece[i] = chunk_piece(p, end, K, share, G);
-          mbar_arrive(smem_u32(&sh.piece_full[i]));
-          if (!share.next(P, K, sh.line, p, end)) break;
-          end += p.t1 - p.t0;
+      PagedPiece p = share.find(P, K, sh.line, share.begin);
+      long long end = share.begin + (p.t1 - p.t0);
+      for (int n = 0;; ++n) {
+        const int i = n % PC_PIECES;
+        ChunkPiece c = chunk_piece(p, end, K, share, G);
+        // pages outside the pool are looked for once per piece
+        const int *table = P.batch.table + (size_t)c.b * P.batch.table_stride;
+        const int last = min(c.keys, c.last_tile() * PC_TK) - 1;
+        bool bad = false;
+#pragma unroll 8
+        for (int pg = (c.u0 * PC_TK >> lg) + lane; pg <= last >> lg; pg += 32) {
+          const int id = table[pg];
+          bad = bad || id < 0 || id >= P.pool.n_pages;
         }
+        c.holes = __any_sync(0xffffffffu, bad);
+        if (!__all_sync(0xffffffffu, pc_wait(smem_u32(&sh.piece_empty[i]), (n / PC_PIECES & 1) ^ 1, &sh.gave_up))) break;
+        if (lane == 0) {
+          sh.piece[i] = c;
+          mbar_arrive(smem_u32(&sh.piece_full[i]));
+        }
+        __syncwarp();
+        if (!share.next(P, K, sh.line, p, end)) break;
+        end += p.t1 - p.t0;
       }
-      __syncwarp();
-    } else if (warp >= 9) {
-      // ---- copies: warp 9 the K tiles, warp 10 the V tiles, which take turns in the ring
-      const int kv = warp - 9;
+    } else if (warp == 10) {
+      // ---- copies: K and V tiles in turn through the ring
       constexpr int PARTS = D / 8;
-      const T *const base = reinterpret_cast<const T *>(kv ? P.pool.v : P.pool.k);
-      const CUtensorMap *const map = &M.map[kv];
       const int rows_here = min(1 << lg, PC_TK);               // of a tile, in one page
       const int n_pages = PC_TK / rows_here;                   // pages of a tile
-      int n = kv;                                              // place in the order of tiles
+      int n = 0;                                               // tiles so far
       bool ok = true;
       ChunkPiece c;
       while (ok && take_piece(c)) {
@@ -224,219 +237,244 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
           return key < n_keys ? table[key >> lg] : -1;
         };
         int ids = look_up(c.u0);
-        for (int i = c.u0; i < end; ++i, n += 2) {
+        for (int i = c.u0; ok && i < end; ++i) {
           const int ids_next = i + 1 < end ? look_up(i + 1) : -1;
-          const int st = n % C::STAGES, left = n_keys - i * PC_TK;
-          ok = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.empty[st]), (n / C::STAGES & 1) ^ 1, &sh.gave_up));
-          if (!ok) break;
-          const uint32_t dst = smem + C::RING + st * C::TILE, bar = smem_u32(&sh.full[st]);
+          const int left = n_keys - i * PC_TK;
           // rows [0, whole) by TMA, the page that the last key shares with rows behind it and nothing else by the lanes
           const int whole = !M.on ? 0 : left >= PC_TK ? PC_TK : left / rows_here * rows_here;
           const int rest = !M.on ? PC_TK : whole < left ? min(PC_TK, whole + rows_here) : whole;          // rows [whole, rest) by the lanes
-          if (lane == 0) mbar_expect_tx(bar, (PC_TK - (rest - whole)) * D * (int)sizeof(T));
-          __syncwarp();
-          if (M.on) {
-            const int panel = lane / n_pages, pg = lane % n_pages, row = pg * rows_here;
-            int id = __shfl_sync(0xffffffffu, ids, row >> 2);
-            if (panel < C::PANELS && (row < whole || row >= rest)) {
-              if (row >= whole || id < 0 || id >= P.pool.n_pages) id = P.pool.n_pages;          // behind the end: zeros
-              tma_page(dst + panel * PC_HALF + row * 128, map, panel * 64, i * PC_TK & ((1 << lg) - 1), c.kvh, id, bar);
-            }
-          }
-          if (rest > whole) {
-            const T *src = base + c.kvh * P.pool.head_stride;
-#pragma unroll 4
-            for (int j = lane; j < (rest - whole) * PARTS; j += 32) {
-              const int row = whole + j / PARTS, part = j % PARTS, key = i * PC_TK + row;
-              const int id = key < n_keys ? table[key >> lg] : -1;
-              const bool real = id >= 0 && id < P.pool.n_pages;
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pc_part(row, part)),
-                           "l"(real ? src + id * P.pool.page_stride + (key & ((1 << lg) - 1)) * P.pool.row_stride + part * 8 : src), "r"(real ? 16 : 0)
-                           : "memory");
-            }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_proxy_async();
+          const int panel = lane / n_pages, row_tma = lane % n_pages * rows_here;
+          int id_tma = __shfl_sync(0xffffffffu, ids, row_tma >> 2);
+          if (row_tma >= whole || id_tma < 0 || id_tma >= P.pool.n_pages) id_tma = P.pool.n_pages;          // behind the end: zeros
+          const bool tma = M.on && panel < C::PANELS && (row_tma < whole || row_tma >= rest);
+#pragma unroll 1
+          for (int kv = 0; kv < 2; ++kv, ++n) {
+            const int st = n % C::STAGES;
+            ok = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.empty[st]), (n / C::STAGES & 1) ^ 1, &sh.gave_up));
+            if (!ok) break;
+            const uint32_t dst = smem + C::RING + st * C::TILE, bar = smem_u32(&sh.full[st]);
+            if (lane == 0) mbar_expect_tx(bar, (PC_TK - (rest - whole)) * D * (int)sizeof(T));
             __syncwarp();
+            if (tma) tma_page(dst + panel * PC_HALF + row_tma * 128, &M.map[kv], panel * 64, i * PC_TK & ((1 << lg) - 1), c.kvh, id_tma, bar);
+            if (rest > whole) {
+              const T *src = reinterpret_cast<const T *>(kv ? P.pool.v : P.pool.k) + c.kvh * P.pool.head_stride;
+#pragma unroll 4
+              for (int j = lane; j < (rest - whole) * PARTS; j += 32) {
+                const int row = whole + j / PARTS, part = j % PARTS, key = i * PC_TK + row;
+                const int id = key < n_keys ? table[key >> lg] : -1;
+                const bool real = id >= 0 && id < P.pool.n_pages;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pc_part(row, part)),
+                             "l"(real ? src + id * P.pool.page_stride + (key & ((1 << lg) - 1)) * P.pool.row_stride + part * 8 : src), "r"(real ? 16 : 0)
+                             : "memory");
+              }
+              asm volatile("cp.async.wait_all;" ::: "memory");
+              fence_proxy_async();
+              __syncwarp();
+            }
+            if (lane == 0) mbar_arrive(bar);
           }
-          if (lane == 0) mbar_arrive(bar);
           ids = ids_next;
         }
         if (c.last) break;
       }
       // leave no copy in flight: the last tiles of a block that gave up get a bounded wait
       if (!ok && lane == 0) {
-        for (int k = max(kv, n - 2 * C::STAGES); k < n; k += 2) {
+        for (int k = max(0, n - C::STAGES); k < n; ++k) {
           const long long t0 = clock64();
           while (!mbar_try_wait(smem_u32(&sh.full[k % C::STAGES]), k / C::STAGES & 1))
             if (clock64() - t0 > PC_WAIT_TICKS) break;
         }
       }
       __syncwarp();
-    } else {
-      // ---- MMA issuer
+    } else if (warp >= 8) {
+      // ---- MMAs of a half
+      const int h = warp - 8;
       constexpr uint32_t fmt = std::is_same<T, __half>::value ? 0u : 1u;
-      const uint32_t idesc_s = (1u << 4) | (fmt << 7) | (fmt << 10) | ((PC_TK >> 3) << 17) | ((PC_M >> 4) << 24);
+      const uint32_t idesc_s = (1u << 4) | (fmt << 7) | (fmt << 10) | ((PC_STEP >> 3) << 17) | ((PC_M >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((D >> 3) << 17) | ((PC_M >> 4) << 24);
-      int st = 0, ph = 0, q_ph = 0, p_ph[2] = {0, 0};
-      bool ok = true;
+      const uint32_t t_s = tmem + h * 128, t_o = tmem + 256 + h * 128;
+      const uint64_t q_desc = pc_desc(smem + C::Q + h * C::TILE, 16);
+      int st = 0, ph = 0, q_ph = 0, o_ph = 0, p_ph = 0, n_pv = 0;          // p_ph: a bit per place; n_pv: P V so far
+      bool ok = true, used = false;                            // used: the half had steps in the piece before
       auto all = [&](bool x) { return __all_sync(0xffffffffu, x); };
       auto commit = [&](uint64_t &bar) {
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&bar)) : "memory");
       };
-      auto scores = [&](int h, int slot) {
-        const uint32_t q = smem + C::Q + h * C::TILE, k = smem + C::RING + slot * C::TILE;
+      auto scores = [&](int slot, int j) {                     // step j: a half of the tile in `slot`
+        const uint64_t k_desc = pc_desc(smem + C::RING + slot * C::TILE + (j & 1) * PC_STEP * 128, 16);
+        const uint32_t d = t_s + (j & 1) * PC_STEP;
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * PC_HALF + (kk & 3) * 32;
-          asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem + h * 128),
-                       "l"(pc_desc(q + off, 16)), "l"(pc_desc(k + off, 16)), "r"(idesc_s), "r"(kk > 0 ? 1u : 0u)
+          const uint64_t off = ((kk >> 2) * PC_HALF + (kk & 3) * 32) >> 4;
+          asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+                       "l"(q_desc + off), "l"(k_desc + off), "r"(idesc_s), "r"(kk > 0 ? 1u : 0u)
                        : "memory");
         }
-        commit(sh.s_full[h]);
+        commit(sh.s_full[h][j & 1]);
       };
-      auto values = [&](int h, int slot, int part, bool first) {           // 64 of the tile's keys
-        const uint32_t v = smem + C::RING + slot * C::TILE;
+      auto values = [&](int slot, int j, bool first, bool last) {
+        const uint64_t v_desc = pc_desc(smem + C::RING + slot * C::TILE + (j & 1) * PC_STEP * 128, PC_HALF);
+        const uint32_t p = t_s + (j & 1) * PC_STEP;
 #pragma unroll
-        for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
-          asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(tmem + 256 + h * 128),
-                       "r"(tmem + h * 128 + kk * 8), "l"(pc_desc(v + kk * 2048, PC_HALF)), "r"(idesc_o), "r"(first && kk == 0 ? 0u : 1u)
+        for (int kk = 0; kk < PC_STEP / 16; ++kk)
+          asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(t_o),
+                       "r"(p + kk * 8), "l"(v_desc + kk * (2048 >> 4)), "r"(idesc_o), "r"(first && kk == 0 ? 0u : 1u)
                        : "memory");
+        commit(sh.o_done[h]);
+        if (last) commit(sh.o_full[h]);
       };
       ChunkPiece c;
       while (ok && take_piece(c)) {
-        const int end = c.last_tile();
-        ok = all(pc_wait(smem_u32(&sh.q_full[0]), q_ph, &sh.gave_up) && pc_wait(smem_u32(&sh.q_full[1]), q_ph, &sh.gave_up));
-        q_ph ^= 1;
-        int k_slot = st;
-        auto advance = [&]() { if (++st == C::STAGES) { st = 0; ph ^= 1; } };
-        auto tile_there = [&]() {
-          ok = ok && all(pc_wait(smem_u32(&sh.full[st]), ph, &sh.gave_up));
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int j0 = 2 * c.u0, end = h ? c.end[1] : c.end[0], n_tiles = c.last_tile() - c.u0;
+        // The ring holds the piece's tiles as K, V, K, V ...; this half needs the first `mine` of each, and lets the others go.
+        const int mine = ((end + 1) >> 1) - c.u0;
+        const int st0 = st, ph0 = ph;
+        auto place_of = [&](int i, int &slot, int &phase) {    // tile i of the piece
+          const int k = st0 + i;
+          slot = k % C::STAGES;
+          phase = ph0 ^ (k / C::STAGES & 1);
         };
-        if (ok && c.u0 < end) {
-          tile_there();
+        auto take_tile = [&](int i) {
+          int slot, phase;
+          place_of(i, slot, phase);
+          ok = ok && all(pc_wait(smem_u32(&sh.full[slot]), phase, &sh.gave_up));
+          return slot;
+        };
+        // the piece before has left both places of S
+        if (used) {
+          ok = ok && all(pc_wait(smem_u32(&sh.o_full[h]), o_ph, &sh.gave_up));
+          o_ph ^= 1;
+        }
+        used = end > j0;
+        if (used) {
+          ok = ok && all(pc_wait(smem_u32(&sh.q_full[h]), q_ph, &sh.gave_up));
+          q_ph ^= 1;
+          int k_slot = take_tile(0), v_slot = 0;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           if (ok && elect_one()) {
-            if (c.u0 < c.end[0]) scores(0, st);
-            if (c.u0 < c.end[1]) scores(1, st);
-            commit(sh.empty[st]);
+            scores(k_slot, j0);
+            if (j0 + 1 < end) scores(k_slot, j0 + 1);
+            commit(sh.empty[k_slot]);
           }
           __syncwarp();
-          advance();
-        }
-        for (int i = c.u0; ok && i < end; ++i) {
-          tile_there();                                        // V of this tile
-          const int v_slot = st;
-          advance();
-          bool k_there = i + 1 >= end;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (i >= c.end[h]) continue;
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-              ok = ok && all(pc_wait(smem_u32(&sh.p_full[h][part]), p_ph[h], &sh.gave_up));
-              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-              if (ok && elect_one()) values(h, v_slot, part, i == c.u0);
-              __syncwarp();
-            }
-            p_ph[h] ^= 1;
-            if (i + 1 < c.end[h]) {
-              if (!k_there) {                                  // K of the next tile
-                tile_there();
-                k_there = true;
-                k_slot = st;
-                advance();
-              }
-              if (ok && elect_one()) scores(h, k_slot);
-            } else {
-              if (ok && elect_one()) commit(sh.o_full[h]);
+          for (int j = j0; ok && j < end; ++j) {
+            if ((j & 1) == 0) v_slot = take_tile(j - j0 + 1);
+            ok = ok && all(pc_wait(smem_u32(&sh.p_full[h][j & 1]), p_ph >> (j & 1) & 1, &sh.gave_up));
+            p_ph ^= 1 << (j & 1);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (ok && elect_one()) {
+              values(v_slot, j, j == j0, j + 1 == end);
+              if ((j & 1) || j + 1 == end) commit(sh.empty[v_slot]);
             }
             __syncwarp();
+            ++n_pv;
+            if (j + 2 < end) {
+              // S of a step goes where P of the second step before lies: behind the end of that P V
+              if ((j & 1) == 0) k_slot = take_tile(j - j0 + 2);
+              ok = ok && all(pc_wait(smem_u32(&sh.o_done[h]), (n_pv - 1) & 1, &sh.gave_up));
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              if (ok && elect_one()) {
+                scores(k_slot, j + 2);
+                if ((j & 1) || j + 3 == end) commit(sh.empty[k_slot]);
+              }
+              __syncwarp();
+            }
           }
-          if (ok && elect_one()) {
-            commit(sh.empty[v_slot]);
-            if (i + 1 < end) commit(sh.empty[k_slot]);
-          }
+        }
+        for (int i = 2 * mine; ok && i < 2 * n_tiles; ++i) {
+          int slot, phase;
+          place_of(i, slot, phase);
+          ok = all(pc_wait(smem_u32(&sh.full[slot]), phase, &sh.gave_up));
+          if (ok && lane == 0) mbar_arrive(smem_u32(&sh.empty[slot]));
           __syncwarp();
         }
+        place_of(2 * n_tiles, st, ph);
         if (c.last) break;
       }
-    }
     } else {
       // ---- softmax: thread = query row = lane of tensor memory
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
       const int h = warp >> 2, row = threadIdx.x & 127, qi = h * PC_M + row;
       const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t t_s = tmem + h * 128 + lane_off, t_o = tmem + 256 + h * 128 + lane_off;
       const float scale = 1.4426950408889634f * rsqrtf((float)D);
-      int s_ph = 0, o_ph = 0;
-      bool ok = true;
-      ChunkPiece c;
-      while (take_piece(c)) {
-        const int nQ = c.rows * G, n_keys = c.keys, end = h ? c.end[1] : c.end[0];
-        const int *table = P.batch.table + (size_t)c.b * P.batch.table_stride;
-        // ---- queries: this half's rows into shared memory (beyond the tile's rows zero)
-        bool holes;
-        {
-          constexpr int PARTS = D / 8, AT_ONCE = 128 / PARTS;
-          const int part = row % PARTS;
-          const T *q = reinterpret_cast<const T *>(P.q);
-          for (int r0 = 0; r0 < PC_M; r0 += AT_ONCE) {
-            const int r = r0 + row / PARTS, i = h * PC_M + r, p = i / G;
-            const bool real = i < nQ;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem + C::Q + h * C::TILE + pc_part(r, part)),
-                         "l"(real ? q + (c.row0 + p) * P.q_stride + (c.kvh * G + i - p * G) * D + part * 8 : q), "r"(real ? 16 : 0)
-                         : "memory");
-          }
-          // pages outside the pool: looked for once per piece
-          bool bad = false;
-          const int last = min(n_keys, c.last_tile() * PC_TK) - 1;
-          for (int pg = (c.u0 * PC_TK >> lg) + (int)threadIdx.x; last >= 0 && pg <= last >> lg; pg += 2 * PC_M) {
-            const int id = table[pg];
-            bad = bad || id < 0 || id >= P.pool.n_pages;
-          }
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          fence_proxy_async();
-          mbar_arrive(smem_u32(&sh.q_full[h]));
-          uint32_t r;
-          asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 256, p;\n selp.u32 %0, 1, 0, q;\n}\n"
-                       : "=r"(r) : "r"((int)bad) : "memory");
-          holes = r != 0;
+      const int my_p = qi / G, my_g = qi - my_p * G;           // position in the tile, head of the group
+      auto has_steps = [&](const ChunkPiece &c) { return (h ? c.end[1] : c.end[0]) > 2 * c.u0; };
+      // this half's rows of a piece into shared memory (beyond the tile's rows zero), if it has steps there
+      auto fetch_queries = [&](const ChunkPiece &c) {
+        if (!has_steps(c)) return;
+        constexpr int PARTS = D / 8, AT_ONCE = 128 / PARTS;
+        const int part = row % PARTS, nQ = c.rows * G;
+        const T *q = reinterpret_cast<const T *>(P.q);
+#pragma unroll 4
+        for (int r0 = 0; r0 < PC_M; r0 += AT_ONCE) {
+          const int r = r0 + row / PARTS, i = h * PC_M + r, p = i / G;
+          const bool real = i < nQ;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem + C::Q + h * C::TILE + pc_part(r, part)),
+                       "l"(real ? q + (c.row0 + p) * P.q_stride + (c.kvh * G + i - p * G) * D + part * 8 : q), "r"(real ? 16 : 0)
+                       : "memory");
         }
-
-        const int seen = qi < nQ ? c.pos + qi / G + 1 : 0;
+      };
+      auto publish_queries = [&](const ChunkPiece &c) {
+        if (!has_steps(c)) return;
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_proxy_async();
+        mbar_arrive(smem_u32(&sh.q_full[h]));
+      };
+      int s_ph = 0, o_ph = 0, n_done = 0;                      // s_ph: a bit per place; n_done: P V so far
+      ChunkPiece c, next;
+      bool ok = take_piece(c);
+      if (ok) {
+        fetch_queries(c);
+        publish_queries(c);
+      }
+      while (ok) {
+        const int j0 = 2 * c.u0, end = h ? c.end[1] : c.end[0], nQ = c.rows * G;
+        const int seen = qi < nQ ? c.pos + my_p + 1 : 0;
         float m = -INFINITY, l = 0.f;
-        for (int i = c.u0; ok && i < end; ++i) {
-          ok = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.s_full[h]), s_ph, &sh.gave_up));
-          s_ph ^= 1;
+        if (j0 == end && !c.last) {
+          ok = take_piece(next);
+          if (!ok) break;
+          fetch_queries(next);
+        }
+        for (int j = j0; j < end; ++j) {
+          ok = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.s_full[h][j & 1]), s_ph >> (j & 1) & 1, &sh.gave_up));
+          s_ph ^= 1 << (j & 1);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          uint32_t s[128];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) tmem_ld32(t_s + 32 * j, *reinterpret_cast<uint32_t(*)[32]>(s + 32 * j));
+          const uint32_t t_here = t_s + (j & 1) * PC_STEP;
+          uint32_t s[PC_STEP];
+          tmem_ld32(t_here, *reinterpret_cast<uint32_t(*)[32]>(s));
+          tmem_ld32(t_here + 32, *reinterpret_cast<uint32_t(*)[32]>(s + 32));
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          const int lim = seen - i * PC_TK;                    // keys of the tile that this row sees
-          if (__any_sync(0xffffffffu, lim < PC_TK)) {
-#pragma unroll
-            for (int j = 0; j < 128; ++j) s[j] = j < lim ? s[j] : 0xff800000u;
+          if (j + 1 == end && !c.last) {                       // the half's last S is computed: its queries may go
+            ok = take_piece(next);
+            if (!ok) break;
+            fetch_queries(next);
           }
-          if (holes) {
+          const int lim = seen - j * PC_STEP;                  // keys of the step that this row sees
+          if (__any_sync(0xffffffffu, lim < PC_STEP)) {
 #pragma unroll
-            for (int j0 = 0; j0 < 128; j0 += 32) {
-              const int key = i * PC_TK + j0 + lane, id = key < n_keys ? table[key >> lg] : -1;
+            for (int k = 0; k < PC_STEP; ++k) s[k] = k < lim ? s[k] : 0xff800000u;
+          }
+          if (c.holes) {
+            const int *table = P.batch.table + (size_t)c.b * P.batch.table_stride;
+#pragma unroll
+            for (int k0 = 0; k0 < PC_STEP; k0 += 32) {
+              const int key = j * PC_STEP + k0 + lane, id = key < c.keys ? table[key >> lg] : -1;
               const uint32_t good = __ballot_sync(0xffffffffu, id >= 0 && id < P.pool.n_pages);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) s[j0 + j] = (good >> j) & 1 ? s[j0 + j] : 0xff800000u;
+              for (int k = 0; k < 32; ++k) s[k0 + k] = (good >> k) & 1 ? s[k0 + k] : 0xff800000u;
             }
           }
           float mx[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) mx[j] = fmaxf(__uint_as_float(s[j]), __uint_as_float(s[j + 4]));
+          for (int k = 0; k < 4; ++k) mx[k] = fmaxf(__uint_as_float(s[k]), __uint_as_float(s[k + 4]));
 #pragma unroll
-          for (int j = 8; j < 128; j += 8) {
+          for (int k = 8; k < PC_STEP; k += 8) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[j + k]), __uint_as_float(s[j + 4 + k]));
+            for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(s[k + i]), __uint_as_float(s[k + 4 + i]));
           }
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+          const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * scale;
           const bool grow = top > m + (PC_ABOVE + LIFT);
           if (__any_sync(0xffffffffu, grow)) {
             float alpha = 1.f;
@@ -445,14 +483,18 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
               m = top - LIFT;
               l *= alpha;
             }
-            if (i > c.u0) {
+            if (j > j0) {
+              // P V of the step before may be under way (the one before that is complete: S of this step was issued behind it)
+              ok = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.o_done[h]), (n_done - 1) & 1, &sh.gave_up));
+              if (!ok) break;
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
               for (int c0 = 0; c0 < D; c0 += 16) {
                 uint32_t o[16];
                 tmem_ld16(t_o + c0, o);
                 asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
                 tmem_st16(t_o + c0, o);
               }
             }
@@ -461,39 +503,37 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
           const uint64_t scale2 = f2_pack(scale, scale), ref2 = f2_pack(-ref, -ref);
           uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-          for (int part = 0; part < 2; ++part) {
+          for (int q = 0; q < 2; ++q) {
+            uint32_t p[16];
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              uint32_t p[16];
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const int k = 64 * part + 32 * q + 2 * j;
-                float a, b;
-                f2_unpack(f2_fma(f2_pack(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), scale2, ref2), a, b);
-                a = exp2_approx(a);
-                b = exp2_approx(b);
-                sum[j & 1] = f2_add(sum[j & 1], f2_pack(a, b));
-                p[j] = Op::pack2(a, b);
-              }
-              tmem_st16(t_s + 32 * part + 16 * q, p);
+            for (int k = 0; k < 16; ++k) {
+              float a, b;
+              f2_unpack(f2_fma(f2_pack(__uint_as_float(s[32 * q + 2 * k]), __uint_as_float(s[32 * q + 2 * k + 1])), scale2, ref2), a, b);
+              a = exp2_approx(a);
+              b = exp2_approx(b);
+              sum[k & 1] = f2_add(sum[k & 1], f2_pack(a, b));
+              p[k] = Op::pack2(a, b);
             }
-            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            mbar_arrive(smem_u32(&sh.p_full[h][part]));
+            tmem_st16(t_here + 16 * q, p);
           }
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          mbar_arrive(smem_u32(&sh.p_full[h][j & 1]));
+          ++n_done;
           float l0, l1;
           f2_unpack(f2_add(sum[0], sum[1]), l0, l1);
           l += l0 + l1;
         }
+        if (ok && !c.last) publish_queries(next);                  // (S of the next piece under the results of this one)
 
         // ---- results
-        const bool any = end > c.u0, whole = c.began && c.ends;
+        const bool any = end > j0, whole = c.began && c.ends;
         if (any && ok) {
           ok = __all_sync(0xffffffffu, pc_wait(smem_u32(&sh.o_full[h]), o_ph, &sh.gave_up));
           o_ph ^= 1;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         }
-        const int p = qi / G, head = c.kvh * G + qi - p * G, place = paged_place(blockIdx.x, c.began);
+        const int head = c.kvh * G + my_g, place = paged_place(blockIdx.x, c.began);
         const float inv = !ok ? NAN : l != 0.f ? 1.f / l : 0.f;
         bool good = true;
         if (!whole && qi < nQ) S.levels<D>(place)[qi] = make_float2(ok ? m : 0.f, ok ? l : NAN);
@@ -507,20 +547,21 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
           if (qi < nQ) {
             float f[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) f[j] = any && l != 0.f ? __uint_as_float(o[j]) : 0.f;
+            for (int k = 0; k < 32; ++k) f[k] = any && l != 0.f ? __uint_as_float(o[k]) : 0.f;
             if (whole) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                f[j] *= inv;
-                good = good && isfinite(f[j]);
+              for (int k = 0; k < 32; ++k) {
+                f[k] *= inv;
+                good = good && isfinite(f[k]);
               }
-              T *dst = reinterpret_cast<T *>(P.out) + ((size_t)(c.row0 + p) * P.nq + head) * D + c0;
+              T *dst = reinterpret_cast<T *>(P.out) + ((size_t)(c.row0 + my_p) * P.nq + head) * D + c0;
 #pragma unroll
-              for (int j = 0; j < 4; ++j) store_pack(dst + 8 * j, *reinterpret_cast<float(*)[8]>(f + 8 * j));
+              for (int k = 0; k < 4; ++k) store_pack(dst + 8 * k, *reinterpret_cast<float(*)[8]>(f + 8 * k));
             } else {
-              float *dst = S.sums<D>(place) + (size_t)qi * D + c0;
+              // four dimensions of all rows after the other: the lanes' values lie side by side
+              float *dst = S.sums<D>(place) + ((size_t)(c0 / 4) * PC_ROWS + qi) * 4;
 #pragma unroll
-              for (int j = 0; j < 8; ++j) store_pack(dst + 4 * j, *reinterpret_cast<float(*)[4]>(f + 4 * j));
+              for (int k = 0; k < 8; ++k) store_pack(dst + (size_t)k * PC_ROWS * 4, *reinterpret_cast<float(*)[4]>(f + 4 * k));
             }
           }
         }
@@ -532,13 +573,14 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
           while (bad_rows) {
             const int i = h * PC_M + (warp & 3) * 32 + __ffs(bad_rows) - 1, r = i / G;
             bad_rows &= bad_rows - 1;
-            paged_attend_row_here<T, T, D>(P, c.b, c.row0 + r, c.pos + r + 1, c.kvh * G + i - r * G);
+            paged_attend_row<T, T, D>(P, c.b, c.row0 + r, c.pos + r + 1, c.kvh * G + i - r * G);
           }
         }
-        if (c.last) {
-          if (threadIdx.x == 0) S.items[blockIdx.x] = PagedCutItem{c.pieces, c.b, c.row0, c.rows, c.pos + 1, c.kvh, {0, 0}};
+        if (c.last || !ok) {
+          if (c.last && threadIdx.x == 0) S.items[blockIdx.x] = PagedCutItem{c.pieces, c.b, c.row0, c.rows, c.pos + 1, c.kvh, {0, 0}};
           break;
         }
+        c = next;
       }
     }
   }

@@ -9,6 +9,8 @@
 // most two of those, one in front and one behind, so scratch has two places to a block.
 #pragma once
 
+#include <type_traits>
+
 #include "paged_attention.cuh"
 
 namespace dmtd {
@@ -209,7 +211,8 @@ struct PagedCutItem {
   int pad[2];
 };
 
-// Scratch: an entry per block, then two partial results per block: [tile rows][D] floats and (level, sum) per row.
+// Scratch: an entry per block, then two partial results per block: [tile rows][D] floats (the chunk kernel: [D / 4][tile
+// rows][4]) and (level, sum) per row.
 struct PagedScratch {
   PagedCutItem *items;
   float *parts;
@@ -222,93 +225,117 @@ struct PagedScratch {
 // A block's place for the piece of an item that began in an earlier block / that goes on in a later one.
 __device__ __forceinline__ int paged_place(int block, bool began_here) { return 2 * block + (began_here ? 1 : 0); }
 
-// Joins query rows q0 .. q0 + AT_ONCE - 1 of the item that is cut at the end of `block`'s share, by one warp.  Levels are powers of
-// two.  The lanes fetch the pieces' levels side by side, and all lanes the pieces' sums, which do not wait for the levels.
-template <typename T, typename KVT, int D, int AT_ONCE, int DEEP>
-__device__ __forceinline__ void paged_join(const PagedAttentionParams &P, const PagedScratch &S, const PagedCutItem &c, int block, int q0) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31, G = P.nq / P.nkv, nQ = c.rows * G;
-  float m[AT_ONCE], l[AT_ONCE], o[AT_ONCE][E];
+// Joins query row qi of the row kernel's item that is cut at the end of `block`'s share, by one warp.  Levels are powers of two.
+// The lanes fetch the pieces' levels side by side, and all lanes the pieces' sums, which do not wait for the levels.
+template <typename T, typename KVT, int D>
+__device__ __forceinline__ void paged_join_row(const PagedAttentionParams &P, const PagedScratch &S, const PagedCutItem &c, int block, int qi) {
+  constexpr int E = D / 32, DEEP = 8;
+  const int lane = threadIdx.x & 31, G = P.nq / P.nkv;
+  float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
-  for (int k = 0; k < AT_ONCE; ++k) {
-    m[k] = -INFINITY;
-    l[k] = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[k][e] = 0.f;
-  }
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
   for (int s0 = 0; s0 < c.pieces; s0 += 32) {
     const int n = min(32, c.pieces - s0);
     auto place = [&](int s) { return paged_place(block + s0 + s, s0 + s == 0); };
-    float2 ml[AT_ONCE];
-    float v[AT_ONCE][DEEP][E], w[AT_ONCE];
+    float v[DEEP][E];
     auto load = [&](int first) {
 #pragma unroll
-      for (int k = 0; k < AT_ONCE; ++k) {
-#pragma unroll
-        for (int s = 0; s < DEEP; ++s)
-          if (first + s < n && q0 + k < nQ) load_pack(S.sums<D>(place(first + s)) + (size_t)(q0 + k) * D + lane * E, v[k][s]);
-      }
+      for (int s = 0; s < DEEP; ++s)
+        if (first + s < n) load_pack(S.sums<D>(place(first + s)) + (size_t)qi * D + lane * E, v[s]);
     };
-#pragma unroll
-    for (int k = 0; k < AT_ONCE; ++k) ml[k] = lane < n && q0 + k < nQ ? S.levels<D>(place(lane))[q0 + k] : make_float2(-INFINITY, 0.f);
+    const float2 ml = lane < n ? S.levels<D>(place(lane))[qi] : make_float2(-INFINITY, 0.f);
     load(0);
+    const float top = fmaxf(m, warp_max(ml.x));
+    const float old = m > -INFINITY ? exp2f(m - top) : 0.f;
+    const float w = ml.x > -INFINITY ? exp2f(ml.x - top) : 0.f;
+    l = l * old + warp_sum(ml.y * w);
+    m = top;
 #pragma unroll
-    for (int k = 0; k < AT_ONCE; ++k) {
-      const float top = fmaxf(m[k], warp_max(ml[k].x));
-      const float old = m[k] > -INFINITY ? exp2f(m[k] - top) : 0.f;
-      w[k] = ml[k].x > -INFINITY ? exp2f(ml[k].x - top) : 0.f;
-      l[k] = l[k] * old + warp_sum(ml[k].y * w[k]);
-      m[k] = top;
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[k][e] *= old;
-    }
+    for (int e = 0; e < E; ++e) o[e] *= old;
     for (int first = 0; first < n; first += DEEP) {
       if (first > 0) load(first);
 #pragma unroll
-      for (int k = 0; k < AT_ONCE; ++k) {
+      for (int s = 0; s < DEEP; ++s) {
+        const float ws = __shfl_sync(0xffffffffu, w, (first + s) & 31);
+        if (first + s < n && ws != 0.f) {
 #pragma unroll
-        for (int s = 0; s < DEEP; ++s) {
-          const float ws = __shfl_sync(0xffffffffu, w[k], (first + s) & 31);
-          if (first + s < n && q0 + k < nQ && ws != 0.f) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[k][e] = fmaf(ws, v[k][s][e], o[k][e]);
-          }
+          for (int e = 0; e < E; ++e) o[e] = fmaf(ws, v[s][e], o[e]);
         }
       }
     }
   }
+  bool good = true;
+  const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-  for (int k = 0; k < AT_ONCE; ++k) {
-    if (q0 + k >= nQ) break;
-    bool good = true;
-    const float inv = l[k] != 0.f ? 1.f / l[k] : 0.f;
+  for (int e = 0; e < E; ++e) {
+    o[e] = l != 0.f ? o[e] * inv : 0.f;
+    good = good && isfinite(o[e]);
+  }
+  const int r = qi / G, row = c.row0 + r, head = c.kvh * G + qi - r * G;
+  if (c.rows > 1 && !__all_sync(0xffffffffu, good)) paged_attend_row<T, KVT, D>(P, c.b, row, c.first_seen + r, head);
+  else store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o);
+}
+
+// Joins 16 dimensions from d0 on of 32 query rows from q0 on of the chunk kernel's item: a lane to a row.
+template <typename T, int D>
+__device__ __forceinline__ void paged_join_rows(const PagedAttentionParams &P, const PagedScratch &S, const PagedCutItem &c, int block, int q0, int d0) {
+  const int lane = threadIdx.x & 31, qi = q0 + lane, G = P.nq / P.nkv;
+  const bool mine = qi < c.rows * G;
+  float m = -INFINITY, l = 0.f, o[16];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      o[k][e] = l[k] != 0.f ? o[k][e] * inv : 0.f;
-      good = good && isfinite(o[k][e]);
-    }
-    const int r = (q0 + k) / G, row = c.row0 + r, head = c.kvh * G + q0 + k - r * G;
-    if (c.rows > 1 && !__all_sync(0xffffffffu, good)) paged_attend_row<T, KVT, D>(P, c.b, row, c.first_seen + r, head);
-    else store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o[k]);
+  for (int e = 0; e < 16; ++e) o[e] = 0.f;
+  for (int s = 0; s < c.pieces && mine; ++s) {                // two or three as a rule
+    const int place = paged_place(block + s, s == 0);
+    float v[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) load_pack(S.sums<D>(place) + ((size_t)(d0 / 4 + k) * S.rows + qi) * 4, v[k]);
+    const float2 ml = S.levels<D>(place)[qi];
+    if (ml.x == -INFINITY) continue;                           // (a piece without keys)
+    const float top = fmaxf(m, ml.x), old = m > -INFINITY ? exp2f(m - top) : 0.f, w = exp2f(ml.x - top);
+    m = top;
+    l = l * old + ml.y * w;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = fmaf(w, v[e / 4][e % 4], o[e] * old);
+  }
+  bool good = true;
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    o[e] = l != 0.f ? o[e] * inv : 0.f;
+    good = good && isfinite(o[e]);
+  }
+  if (mine) {
+    const int r = qi / G;
+    T *dst = reinterpret_cast<T *>(P.out) + ((size_t)(c.row0 + r) * P.nq + c.kvh * G + qi - r * G) * D + d0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) store_pack(dst + 8 * k, *reinterpret_cast<float(*)[8]>(o + 8 * k));
+  }
+  uint32_t bad_rows = __ballot_sync(0xffffffffu, mine && !good && c.rows > 1);
+  __syncwarp();
+  while (bad_rows) {
+    const int i = q0 + __ffs(bad_rows) - 1, r = i / G;
+    bad_rows &= bad_rows - 1;
+    paged_attend_row<T, T, D>(P, c.b, c.row0 + r, c.first_seen + r, c.kvh * G + i - r * G);
   }
 }
 
 // Joins what was cut: a block to each of the row kernel's `blocks` shares, a warp to a row; then, if the chunk kernel ran
-// too, 256 / PAGED_MERGE_ROWS blocks to each of its shares, a warp to four rows (items of it are cut into two or three as a rule).
-constexpr int PAGED_MERGE_WARPS = 16, PAGED_MERGE_ROWS = PAGED_MERGE_WARPS * 4;
+// too, per_chunk blocks to each of its shares.
+constexpr int PAGED_MERGE_WARPS = 16;
+template <int D> __host__ __device__ constexpr int paged_merge_per_chunk(int rows) { return rows / 32 * (D / 16) / PAGED_MERGE_WARPS; }
 template <typename T, typename KVT, int D>
-__global__ void __launch_bounds__(PAGED_MERGE_WARPS * 32, 2) paged_merge_kernel(const __grid_constant__ PagedAttentionParams P, PagedScratch S,
-                                                                                 int blocks, PagedScratch S_chunk) {
+__global__ void __launch_bounds__(PAGED_MERGE_WARPS * 32) paged_merge_kernel(const __grid_constant__ PagedAttentionParams P, PagedScratch S, int blocks,
+                                                                              PagedScratch S_chunk) {
   paged_enter();
-  const int warp = threadIdx.x >> 5;
+  const int warp = threadIdx.x >> 5, G = P.nq / P.nkv;
   if ((int)blockIdx.x < blocks) {
     const PagedCutItem c = S.items[blockIdx.x];
-    if (c.pieces && warp < c.rows * (P.nq / P.nkv)) paged_join<T, KVT, D, 1, 8>(P, S, c, blockIdx.x, warp);
-  } else {
-    const int per = S_chunk.rows / PAGED_MERGE_ROWS, block = (blockIdx.x - blocks) / per, part = (blockIdx.x - blocks) % per;
+    if (c.pieces && warp < c.rows * G) paged_join_row<T, KVT, D>(P, S, c, blockIdx.x, warp);
+  } else if constexpr (std::is_same<T, KVT>::value) {
+    const int per = paged_merge_per_chunk<D>(S_chunk.rows), block = (blockIdx.x - blocks) / per;
+    const int task = (blockIdx.x - blocks) % per * PAGED_MERGE_WARPS + warp, q0 = task / (D / 16) * 32;
     const PagedCutItem c = S_chunk.items[block];
-    const int q0 = (part * PAGED_MERGE_WARPS + warp) * 4;
-    if (c.pieces && q0 < c.rows * (P.nq / P.nkv)) paged_join<T, KVT, D, 4, 2>(P, S_chunk, c, block, q0);
+    if (c.pieces && q0 < c.rows * G) paged_join_rows<T, D>(P, S_chunk, c, block, q0, task % (D / 16) * 16);
   }
 }
 

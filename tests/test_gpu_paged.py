@@ -295,6 +295,8 @@ TYPES = [(F32, F32), (F32, BF16), (F32, F16), (BF16, BF16), (F16, F16)]
     (8, 2, 128, 16, "hnd", [0, 100, 250], [130, 33, 17]),                # pieces of prompts
     (16, 8, 64, 128, "nhd", [0, 640], [257, 1]),
     (32, 2, 128, 16, "hnd", [40, 0, 9], [1, 70, 2]),                     # 16 heads to a group
+    (32, 8, 128, 16, "hnd", [3000], [700]),                              # items cut where one half of their rows sees no more keys
+    (16, 8, 64, 64, "nhd", [1500, 2100, 0], [300, 211, 190]),
 ])
 def test_attention(pkg, qt, kv, nq, nkv, D, page, layout, cached, new):
     c = attention_case(1, cached, new, nq, nkv, D, qt, kv, page, layout, pad=3, q_room=16)

@@ -358,22 +358,24 @@ PAGED_ATTENTION_SCRATCH_BYTES = 48 << 20
 PagedPlan = namedtuple("PagedPlan", "row_start position slot granted lens n_free")
 
 
-def _here(*tensors):
-    """Every tensor is on the current device, whose current stream the call runs on."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        assert t is None or t.get_device() == dev, f"a tensor on {t.device}, the current device is cuda:{dev}"
+_native = None
 
 
-def _ints(*tensors):
-    for t in tensors:
-        assert t.dtype == torch.int32 and t.is_contiguous(), (t.dtype, t.stride())
+def _paged():
+    """The argument marshalling of the calls below, compiled (csrc/paged_binding.cpp)."""
+    global _native
+    if _native is None:
+        load_library()
+        try:
+            from . import _paged as native
+        except ImportError as e:
+            raise DmtdError(STATUS["UNSUPPORTED"], f"{e}: build it with `python -m paper_2510_11958_b200.build`") from e
+        _native = native
+    return _native
 
 
-def _paged_cache(k, v):
-    assert k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1 and k.dtype == v.dtype
-    (n_pages, nkv, page, D), (s_page, s_head, s_row, _) = k.shape, k.stride()
-    return C.byref(_PagedCache(k.data_ptr(), v.data_ptr(), _KV_CODE[k.dtype], n_pages, page, nkv, D, s_page, s_head, s_row))
+def _failed(rc):
+    raise DmtdError(rc, load_library().dmtd_last_error(None).decode())
 
 
 def paged_plan(lens, n_new, table, free_pages, n_free, page_size, n_rows, out=None):
@@ -383,19 +385,13 @@ def paged_plan(lens, n_new, table, free_pages, n_free, page_size, n_rows, out=No
     int32 [pages of the pool], of which the first n_free (cuda int32 [1]) are free, updated in place.  `out`: the
     six tensors to write to (lens and n_free may be the ones read); without it they are allocated.
     """
-    dll = _dll or load_library()
-    B, width = table.shape
     if out is None:
+        B = table.shape[0]
         out = [torch.empty(n, dtype=torch.int32, device=lens.device) for n in (B + 1, n_rows, n_rows, B, B, 1)]
-    _here(lens, n_new, table, free_pages, n_free, *out)
-    _ints(lens, n_new, table, free_pages, n_free, *out)
-    assert lens.numel() == n_new.numel() == B and n_free.numel() == 1
-    assert tuple(t.numel() for t in out) == (B + 1, n_rows, n_rows, B, B, 1)
-    rc = dll.dmtd_paged_plan(lens.data_ptr(), n_new.data_ptr(), B, page_size, table.data_ptr(), width, free_pages.data_ptr(),
-                             free_pages.numel(), n_free.data_ptr(), n_rows, *(t.data_ptr() for t in out), _current_stream())
+    rc = (_native or _paged()).plan(lens, n_new, table, free_pages, n_free, page_size, n_rows, *out)
     if rc:
-        raise DmtdError(rc, dll.dmtd_last_error(None).decode())
-    return PagedPlan(*out)
+        _failed(rc)
+    return PagedPlan._make(out)
 
 
 def paged_append(q, k, v, position, slot, k_cache, v_cache, q_norm=None, k_norm=None, eps=1e-6, rope_theta=0.0, q_out=None):
@@ -405,27 +401,11 @@ def paged_append(q, k, v, position, slot, k_cache, v_cache, q_norm=None, k_norm=
     apart; position, slot: cuda int32 [T] (PagedPlan); k_cache, v_cache: cuda [pages, nkv, page_size, D] in any order in
     memory; q_norm, k_norm: cuda float32 [D] or None.  Rows without a slot are left alone, in q_out too.
     """
-    dll = _dll or load_library()
-    T, nkv, D = k.shape
-    nq = 0 if q is None else q.shape[1]
-    if q is not None and q_out is None:
+    if q_out is None and q is not None:
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _here(q, k, v, position, slot, k_cache, v_cache, q_norm, k_norm, q_out)
-    _ints(position, slot)
-    assert position.numel() == T and slot.numel() == T and v.shape == k.shape and v.dtype == k.dtype
-    assert k_cache.shape[1] == nkv and k_cache.shape[3] == D
-    for t in (q, k, v):
-        assert t is None or (t.shape[0] == T and t.shape[2] == D and t.dtype == k.dtype and t.stride(2) == 1 and t.stride(1) == D)
-    for t in (q_norm, k_norm):
-        assert t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == D)
-    assert q is None or (q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.is_contiguous())
-    rc = dll.dmtd_paged_append(None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), _KV_CODE[k.dtype],
-                               0 if q is None else q.stride(0), k.stride(0), v.stride(0), T, nq,
-                               None if q_norm is None else q_norm.data_ptr(), None if k_norm is None else k_norm.data_ptr(), eps, rope_theta,
-                               position.data_ptr(), slot.data_ptr(), _paged_cache(k_cache, v_cache),
-                               None if q is None else q_out.data_ptr(), _current_stream())
+    rc = (_native or _paged()).append(q, k, v, position, slot, k_cache, v_cache, q_norm, k_norm, eps, rope_theta, q_out)
     if rc:
-        raise DmtdError(rc, dll.dmtd_last_error(None).decode())
+        _failed(rc)
     return q_out
 
 
@@ -435,22 +415,13 @@ def paged_attention(q, row_start, lens, table, k_cache, v_cache, max_new=0, scra
     q: cuda [T, nq, D], float32 with any cache or of the cache's 16-bit type, rows any multiple of 16 bytes apart; row_start:
     cuda int32 [B + 1], lens: cuda int32 [B] with the new rows counted, table: cuda int32 [B, pages] (PagedPlan); k_cache,
     v_cache as in paged_append.  Rows of no request are left as they were in `out` (allocated if not given).
-    `scratch`: a cuda uint8 tensor of PAGED_ATTENTION_SCRATCH_BYTES bytes, allocated through torch if not given.
+    `scratch`: a cuda tensor of PAGED_ATTENTION_SCRATCH_BYTES bytes or more, allocated through torch if not given.
     """
-    dll = _dll or load_library()
-    T, nq, D = q.shape
-    B, width = table.shape
     if scratch is None:
         scratch = torch.empty(PAGED_ATTENTION_SCRATCH_BYTES, dtype=torch.uint8, device=q.device)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _here(q, row_start, lens, table, k_cache, v_cache, scratch, out)
-    _ints(row_start, lens, table)
-    assert row_start.numel() == B + 1 and lens.numel() == B and k_cache.shape[3] == D and scratch.is_contiguous()
-    assert q.stride(2) == 1 and q.stride(1) == D and out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
-    rc = dll.dmtd_paged_attention(q.data_ptr(), _KV_CODE[q.dtype], q.stride(0), T, nq, row_start.data_ptr(), lens.data_ptr(), B,
-                                  table.data_ptr(), width, max_new, _paged_cache(k_cache, v_cache), scratch.data_ptr(),
-                                  scratch.numel() * scratch.element_size(), out.data_ptr(), _current_stream())
+    rc = (_native or _paged()).attention(q, row_start, lens, table, k_cache, v_cache, max_new, scratch, out)
     if rc:
-        raise DmtdError(rc, dll.dmtd_last_error(None).decode())
+        _failed(rc)
     return out

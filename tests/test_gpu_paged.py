@@ -500,3 +500,31 @@ def test_against_the_contiguous_cache(pkg):
     got = check_attention(pkg, c).view(B, R, nq, D)
     # that call rounds queries and probabilities to fp16
     assert (got - want).abs().max() <= 4 * 2.0 ** -12 * max(1.0, want.abs().max().item())
+
+
+def test_tensors_of_the_wrong_kind_are_refused(pkg):
+    c = attention_case(10, [20], [2], 8, 2, 64, BF16, BF16, 16, "hnd")
+    start, lens, table, kc, vc, q = ints(c["start"]), ints(c["lens"]), c["table"], c["kc"], c["vc"], c["q"]
+    for args in ((q.double(), start, lens, table, kc, vc), (q, start.long(), lens, table, kc, vc), (q, start, lens, table[0], kc, vc),
+                 (q, start[:1], lens, table, kc, vc), (q, start, lens, table, kc, vc[:1]), (q, start, lens, table, kc, vc.float()),
+                 (q.transpose(0, 1), start, lens, table, kc, vc), (q[..., :32], start, lens, table, kc, vc),
+                 (q, start, lens, torch.zeros(2, 4, dtype=torch.int32, device="cuda").t()[:1], kc, vc)):
+        with pytest.raises(ValueError):
+            pkg.paged_attention(*args)
+    with pytest.raises(ValueError):
+        pkg.paged_attention(q, start, lens, table, kc, vc, out=torch.empty(2, 8, 64, device="cuda"))
+    with pytest.raises(pkg.DmtdError) as e:
+        pkg.paged_attention(q, start, lens, table, kc, vc, scratch=torch.empty(1 << 20, device="cuda"))
+    assert "scratch" in str(e.value)
+    k = torch.zeros(2, 2, 64, device="cuda")
+    pos = ints([0, 1])
+    for args, kw in (((None, k, k.half(), pos, pos, kc, vc), {}), ((None, k, k, pos.long(), pos, kc, vc), {}), ((None, k[:, :1], k[:, :1], pos, pos, kc, vc), {}),
+                     ((None, k, k, pos, pos, kc, vc), {"k_norm": torch.ones(32, device="cuda")}),
+                     ((k, k, k, pos, pos, kc, vc), {"q_out": k.half()}), ((None, k, k, pos[:1], pos, kc, vc), {})):
+        with pytest.raises(ValueError):
+            pkg.paged_append(*args, **kw)
+    i = ints([0, 0])
+    with pytest.raises(ValueError):
+        pkg.paged_plan(i, ints([0]), table.repeat(2, 1), i, ints([1]), 16, 4)
+    with pytest.raises(ValueError):
+        pkg.paged_plan(i, i, table.repeat(2, 1), i, ints([1]), 16, 4, out=[i] * 6)

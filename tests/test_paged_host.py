@@ -107,3 +107,21 @@ def test_the_header_and_the_binding_agree(dll):
     fields = re.search(r"typedef struct \{([^}]*)\} dmtd_paged_cache;", re.sub(r"/\*.*?\*/", "", text, flags=re.S)).group(1)
     names = [n.strip(" *\n") for part in fields.split(";") for n in re.sub(r"^\s*(void|int32_t|int64_t)\s", "", part).split(",")]
     assert [n for n in names if n] == [n for n, _ in _PagedCache._fields_]
+
+
+def test_tensors_off_the_device_are_refused(dll):
+    """Argument marshalling: CPU tensors, wrong counts of arguments (what needs CUDA tensors is tested on a GPU)."""
+    import torch
+    i = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="table is not on the current CUDA device"):
+        pkg.paged_plan(i, i, torch.zeros(2, 3, dtype=torch.int32), i, i[:1], 16, 4, out=[i] * 6)
+    k = torch.zeros(3, 2, 16, 64)
+    with pytest.raises(ValueError, match="k_cache is not on the current CUDA device"):
+        pkg.paged_append(None, k[0], k[0], i, i, k, k)
+    with pytest.raises(ValueError, match="k_cache is not"):
+        pkg.paged_attention(k[0], i, i, i[None], k, k, scratch=i, out=k[0])
+    from paper_2510_11958_b200 import binding
+    with pytest.raises(TypeError, match="13 wanted"):
+        binding._paged().plan(i)
+    with pytest.raises(ValueError, match="is no tensor"):
+        binding._paged().attention(*[None] * 9)

@@ -17,6 +17,8 @@ dmtd_status launched(cudaError_t e, const char *what) {
   return e == cudaSuccess ? DMTD_OK : call_failed(DMTD_ERR_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
 }
 
+constexpr int APPEND_LEAST_WARPS = 2000;
+
 size_t dtype_bytes(int t) { return t == DMTD_F32 ? 4 : 2; }
 bool known_dtype(int t) { return t == DMTD_F32 || t == DMTD_BF16 || t == DMTD_F16; }
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -47,13 +49,13 @@ dmtd_status pool_check(const char *what, const dmtd_paged_cache *c, PagedPool *o
   return DMTD_OK;
 }
 
-template <int D, int ROWS>
-cudaError_t append_launch(const PagedAppendParams &P, int act, int kv, dim3 grid, cudaStream_t stream) {
-  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(APPEND_THREADS), 0, stream, P); };
+template <int D>
+cudaError_t append_launch(const PagedAppendParams &P, int act, int kv, int blocks, cudaStream_t stream) {
+  auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(blocks), dim3(APPEND_THREADS), APPEND_SMEM, stream, P); };
   auto by_kv = [&](auto t) {
     using T = decltype(t);
-    return kv == DMTD_F32 ? go(paged_append_kernel<T, float, D, ROWS>)
-         : kv == DMTD_BF16 ? go(paged_append_kernel<T, __nv_bfloat16, D, ROWS>) : go(paged_append_kernel<T, __half, D, ROWS>);
+    return kv == DMTD_F32 ? go(paged_append_kernel<T, float, D>)
+         : kv == DMTD_BF16 ? go(paged_append_kernel<T, __nv_bfloat16, D>) : go(paged_append_kernel<T, __half, D>);
   };
   return act == DMTD_F32 ? by_kv(float{}) : act == DMTD_BF16 ? by_kv(__nv_bfloat16{}) : by_kv(__half{});
 }
@@ -169,15 +171,21 @@ dmtd_status dmtd_paged_plan(const int32_t *lens, const int32_t *n_new, int32_t n
   if (n_requests > PLAN_MAX_REQUESTS) return call_failed(DMTD_ERR_CAPACITY, "paged_plan: more than %d requests", PLAN_MAX_REQUESTS);
   if (((int64_t)n_pages << lg) > INT32_MAX || n_pages >= PLAN_MOST || n_rows >= PLAN_MOST || (int64_t)n_requests * table_stride >= PLAN_MOST)
     return call_failed(DMTD_ERR_CAPACITY, "paged_plan: more than 2^31 - 1 slots, or 2^30 rows or table entries");
+  const bool fill = n_rows <= 16384;
   const PagedPlanParams P{lens, n_new, n_requests, lg, table, table_stride, free_pages, n_pages, n_free, n_rows,
-                          row_start, position, slot, granted, lens_out, n_free_out};
+                          row_start, position, slot, granted, lens_out, n_free_out, fill};
   const int smem = plan_smem_bytes(n_requests);
   cudaError_t e = cudaSuccess;
   if (smem > 48 * 1024) e = cudaFuncSetAttribute(paged_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return call_failed(DMTD_ERR_CUDA, "paged_plan: %s", cudaGetErrorString(e));
-  const int ranks = n_rows > 4 * PLAN_THREADS || n_requests > PLAN_THREADS ? PLAN_CLUSTER : 1;
-  return launched(launch_cluster(paged_plan_kernel, dim3(ranks), dim3(PLAN_THREADS), smem, static_cast<cudaStream_t>(cuda_stream), ranks, P),
-                  "paged_plan");
+  // few requests: few warps, whose scans are the shorter ones
+  const int ranks = n_rows > PLAN_THREADS || n_requests > PLAN_THREADS ? PLAN_CLUSTER : 1;
+  const int threads = n_requests > 512 || n_rows > 8 * 512 * PLAN_CLUSTER ? PLAN_THREADS : n_requests > 128 || n_rows > 512 ? 512 : 128;
+  e = launch_cluster(paged_plan_kernel, dim3(ranks), dim3(threads), smem, static_cast<cudaStream_t>(cuda_stream), ranks, P);
+  if (e == cudaSuccess && !fill)
+    e = launch_pdl(paged_rows_of_plan_kernel, dim3((n_rows + PLAN_FILL - 1) / PLAN_FILL), dim3(PLAN_FILL), (n_requests + 1) * 4,
+                   static_cast<cudaStream_t>(cuda_stream), P);
+  return launched(e, "paged_plan");
 }
 
 dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32_t dtype, int64_t q_stride, int64_t k_stride,
@@ -203,25 +211,21 @@ dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32
   P.q_stride = q_stride; P.k_stride = k_stride; P.v_stride = v_stride;
   P.n_rows = n_rows; P.nq = n_q_heads; P.nkv = nkv;
   P.q_norm = q_norm; P.k_norm = k_norm; P.eps = rms_eps;
-  P.rotate = rope_theta > 0.f;
   P.position = position; P.slot = slot; P.q_out = q_out;
-  if (P.rotate) {
+  if (rope_theta > 0.f) {                                // (else all angles are 0)
     const double ratio = std::pow((double)rope_theta, -2.0 / D);
     double f = 0.15915494309189533577;                   // 1 / (2 pi)
     for (int i = 0; i < D / 2; ++i, f *= ratio) P.turns[i] = f;
   }
-  const int n_vec = n_q_heads + 2 * nkv;
+  // a row to a warp; fewer rows than make some 2000 warps are cut, as far as to a vector for every group of threads
+  const int n_vec = n_q_heads + 2 * nkv, at_once = 32 / (D / 2 / (int)unit), most = (n_vec + at_once - 1) / at_once;
+  P.slices = std::min(most, std::max(1, APPEND_LEAST_WARPS / n_rows));
+  P.per_slice = (most + P.slices - 1) / P.slices * at_once;
+  P.slices = (n_vec + P.per_slice - 1) / P.per_slice;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  cudaError_t e;
-  if (n_rows >= 600) {
-    P.per_block = n_vec;
-    const dim3 grid((n_rows + APPEND_ROWS - 1) / APPEND_ROWS, 1);
-    e = D == 128 ? append_launch<128, APPEND_ROWS>(P, dtype, cache->dtype, grid, stream) : append_launch<64, APPEND_ROWS>(P, dtype, cache->dtype, grid, stream);
-  } else {
-    P.per_block = std::min(n_vec, 16);
-    const dim3 grid(n_rows, (n_vec + P.per_block - 1) / P.per_block);
-    e = D == 128 ? append_launch<128, 1>(P, dtype, cache->dtype, grid, stream) : append_launch<64, 1>(P, dtype, cache->dtype, grid, stream);
-  }
+  const int64_t warps = (int64_t)n_rows * P.slices, blocks = (warps + APPEND_WARPS - 1) / APPEND_WARPS;
+  if (warps > INT32_MAX - APPEND_WARPS) return call_failed(DMTD_ERR_CAPACITY, "paged_append: too many rows");
+  const cudaError_t e = D == 128 ? append_launch<128>(P, dtype, cache->dtype, (int)blocks, stream) : append_launch<64>(P, dtype, cache->dtype, (int)blocks, stream);
   return launched(e, "paged_append");
 }
 

@@ -26,10 +26,12 @@ NAMES = ["qkv_pro", "qkv_mma", "qkv_bar", "attn", "-", "attn_bar", "o_pro", "o_m
 
 
 def build_timing_library():
+    sys.path.insert(0, ROOT)
+    from paper_2510_11958_b200.build import SOURCES
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
            "-DDMTD_PASS_TIMING", "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"),
-           os.path.join(HERE, "csrc", "engine.cu"), "-o", LIB] + os.environ.get("DMTD_NVCC_FLAGS", "").split()
+           *(os.path.join(HERE, "csrc", f) for f in SOURCES), "-o", LIB] + os.environ.get("DMTD_NVCC_FLAGS", "").split()
     subprocess.run(cmd, check=True)
     return LIB
 

@@ -82,6 +82,7 @@ def plan_case(seed, B, page, width, most_new, pad, short, ended, holes):
     (1024, 16, 20, 3, 0, False, 0.1, False),          # the last size of one block's one round
     (1025, 16, 20, 3, 1, False, 0.0, False),
     (8192, 4, 16, 9, 100, True, 0.05, True),          # the most requests
+    (3000, 16, 20, 40, 7, True, 0.1, True),           # more than 16384 rows: a second launch writes them
 ])
 def test_plan(pkg, B, page, width, most_new, pad, short, ended, holes):
     for seed in range(3):

@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
     };
     if (warp == 11) {
       // ---- the list of pieces
-      PagedPiece p = share.find(P, K, sh.line, share.begin);
+      PagedPiece p = sh.line.first;
       long long end = share.begin + (p.t1 - p.t0);
       for (int n = 0;; ++n) {
         const int i = n % PC_PIECES;

@@ -17,16 +17,21 @@ namespace dmtd {
 
 // Sum of floor((a i + b) / m) over i = 0 .. n - 1, by exchanging the roles of i and the quotient (a lattice-point
 // count under a line, as in Euclid's algorithm).
-__device__ __forceinline__ long long floor_sum(unsigned long long n, unsigned long long m, unsigned long long a, unsigned long long b) {
-  unsigned long long s = 0;
+__device__ __forceinline__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned long long b) {
+  long long s = 0;
   for (;;) {
-    if (a >= m) { s += n * (n - 1) / 2 * (a / m); a %= m; }
-    if (b >= m) { s += n * (b / m); b %= m; }
-    const unsigned long long y = a * n + b;
-    if (y < m) return (long long)s;
-    n = y / m;
-    b = y % m;
-    const unsigned long long t = m; m = a; a = t;
+    if (a >= m) { s += (long long)n * (n - 1) / 2 * (a / m); a %= m; }
+    if (b >= m) {
+      const unsigned long long q = b >> 32 ? b / m : (unsigned)b / m;
+      s += (long long)(n * q);
+      b -= q * m;
+    }
+    const unsigned long long y = (unsigned long long)a * n + b;
+    if (y < m) return s;
+    const unsigned long long q = y >> 32 ? y / m : (unsigned)y / m;
+    b = y - q * m;
+    n = (unsigned)q;
+    const unsigned t = m; m = a; a = t;
   }
 }
 
@@ -58,7 +63,7 @@ struct PagedRequest {
     const int none = c < 0 ? min(full, (int)(-(long long)c / K.tile)) : 0;       // tiles in front of position 0
     long long s = full;
     if (full > none)
-      s += floor_sum(full - none, 1ull << K.lg_unit, K.tile, (long long)c + (long long)(none + 1) * K.tile + (1 << K.lg_unit) - 1);
+      s += floor_sum(full - none, 1u << K.lg_unit, K.tile, (long long)c + (long long)(none + 1) * K.tile + (1 << K.lg_unit) - 1);
     return m > full ? s + units(K, full) : s;
   }
 };
@@ -98,7 +103,8 @@ struct PagedShare {
   long long each, rest;              // a share's units: `each`, and `rest` of the shares have one more
   int n_blocks;
   struct Shared {
-    long long upto[THREADS];         // units of the threads' requests up to and with a thread's own
+    long long warp_units[THREADS / 32];
+    PagedPiece first;                // the share's first piece, by plan()
     int kept[KEPT][3];               // row0, n, c
   };
   __device__ __forceinline__ PagedRequest request(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, int b) const {
@@ -112,13 +118,15 @@ struct PagedShare {
     return r;
   }
 
-  // Whole block; `sh` in shared memory.
+  // Whole block; `sh` in shared memory.  The threads' requests follow each other on the line; the thread among whose requests the
+  // share begins works out its first piece.
   __device__ __forceinline__ void plan(const PagedAttentionParams &P, const PagedCut &K, Shared &sh, int block, int grid) {
-    const int B = P.batch.n_requests, per = (B + THREADS - 1) / THREADS, b0 = threadIdx.x * per;
-    long long mine = 0;
+    const int B = P.batch.n_requests, per = (B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, warp = threadIdx.x >> 5;
+    long long mine = 0, upto = 0;
+    PagedRequest r{};
     if (threadIdx.x < THREADS) {
       for (int b = b0; b < min(B, b0 + per); ++b) {
-        const PagedRequest r = paged_request(P.batch, P.pool.lg_page, K, b);
+        r = paged_request(P.batch, P.pool.lg_page, K, b);
         mine += r.units_before(K, r.tiles) * P.nkv;
         if (B <= KEPT) {
           sh.kept[b][0] = r.row0;
@@ -126,28 +134,40 @@ struct PagedShare {
           sh.kept[b][2] = r.c;
         }
       }
-      // within a warp, then over the warps
+      upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long w = __shfl_up_sync(0xffffffffu, mine, o);
-        if ((threadIdx.x & 31) >= o) mine += w;
+        const long long w = __shfl_up_sync(0xffffffffu, upto, o);
+        if ((threadIdx.x & 31) >= o) upto += w;
       }
-      sh.upto[threadIdx.x] = mine;
+      if ((threadIdx.x & 31) == 31) sh.warp_units[warp] = upto;
     }
     __syncthreads();
-    if (threadIdx.x < THREADS) {
-      for (int w = 0; w < (int)(threadIdx.x >> 5); ++w) mine += sh.upto[w * 32 + 31];
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < warp) upto += sh.warp_units[w];
+      total += sh.warp_units[w];
     }
-    __syncthreads();
-    if (threadIdx.x < THREADS) sh.upto[threadIdx.x] = mine;
-    __syncthreads();
-    total = sh.upto[THREADS - 1];
     // no empty shares: the pieces of an item are consecutive blocks
     n_blocks = (int)min((long long)grid, quotient(total + K.least - 1, K.least));
     each = n_blocks ? quotient(total, n_blocks) : 0;
     rest = total - each * n_blocks;
     begin = block < n_blocks ? start(block) : total;
     end = block < n_blocks ? start(block + 1) : total;
+    if (threadIdx.x < THREADS && begin < end && upto - mine <= begin && begin < upto) {
+      long long v = begin - (upto - mine);
+      if (per > 1) {
+        for (int b = b0;; ++b) {
+          r = request(P, K, sh, b);
+          const long long all = r.units_before(K, r.tiles) * P.nkv;
+          if (v < all || b + 1 >= B) break;
+          v -= all;
+        }
+      }
+      sh.first = piece_of(P, K, r, v);
+    }
+    __syncthreads();
   }
   __device__ __forceinline__ long long start(int block) const { return each * block + min((long long)block, rest); }
   // the block that holds unit u
@@ -156,34 +176,22 @@ struct PagedShare {
     return (int)(u < longer ? quotient(u, each + 1) : rest + quotient(u - longer, each));
   }
 
-  // The piece that begins at unit u of the line (u < end).
-  __device__ __forceinline__ PagedPiece find(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, long long u) const {
-    int lo = 0, hi = THREADS - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (sh.upto[mid] > u) hi = mid; else lo = mid + 1;
-    }
-    const int B = P.batch.n_requests, per = (B + THREADS - 1) / THREADS;
-    long long v = u - (lo ? sh.upto[lo - 1] : 0);
+  // The piece that begins with the share, at unit v of request r.
+  __device__ __forceinline__ PagedPiece piece_of(const PagedAttentionParams &P, const PagedCut &K, const PagedRequest &r, long long v) const {
     PagedPiece p;
-    for (int b = lo * per;; ++b) {
-      p.r = request(P, K, sh, b);
-      const long long all = p.r.units_before(K, p.r.tiles) * P.nkv;
-      if (v < all || b + 1 >= B) break;
-      v -= all;
-    }
+    p.r = r;
     // the row tile: the last whose units begin at or before v
     int t = 0;
-    for (int top = p.r.tiles; top - t > 1;) {
+    for (int top = r.tiles; top - t > 1;) {
       const int mid = (t + top) >> 1;
-      if (p.r.units_before(K, mid) * P.nkv <= v) t = mid; else top = mid;
+      if (r.units_before(K, mid) * P.nkv <= v) t = mid; else top = mid;
     }
-    v -= p.r.units_before(K, t) * P.nkv;
+    if (t) v -= r.units_before(K, t) * P.nkv;
     p.i = t;
-    p.per_item = p.r.units(K, t);
+    p.per_item = r.units(K, t);
     p.kvh = (int)quotient(v, p.per_item);
     p.t0 = (int)(v - (long long)p.kvh * p.per_item);
-    p.t1 = (int)min((long long)p.per_item, p.t0 + (end - u));
+    p.t1 = (int)min((long long)p.per_item, p.t0 + (end - begin));
     return p;
   }
   // The piece behind p, which ends at unit u of the line; false: the share ends there.

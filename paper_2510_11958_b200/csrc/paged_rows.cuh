@@ -10,8 +10,8 @@
 // Softmax.  A row's probabilities are relative to a reference that is raised only when a score lies more than 2^6 above it (as
 // the first one does): in between, a tile needs no maximum over the lanes and no scaling of the sums, and the exponentials do not wait for one.
 //
-// Types.  16-bit queries: one product each for Q K^T and P V, probabilities rounded once to the cache's type.  fp32
-// queries: queries and probabilities as two fp16 or three bf16 parts, exact to 2^-22 and 2^-24, a product per part; the cache's values
+// Types.  16-bit queries: one product for Q K^T, two for P V, probabilities in two parts (with one, rounded as the result is, the
+// error of the result is 1.4 times that of its own rounding).  fp32 queries: queries and probabilities as two fp16 or three bf16 parts, exact to 2^-22 and 2^-24, a product per part; the cache's values
 // are exact as they are.  fp32 cache: everything in two tf32 parts (2^-22), three products.
 //
 // Bound: KV bytes.  An SM's share of HBM is a tile in 360 cycles; its arithmetic takes 260 (32 MMAs) with 16-bit queries.
@@ -57,6 +57,7 @@ template <typename T, typename KVT, int D>
 struct RowsTypes {
   static constexpr bool TF32 = std::is_same<KVT, float>::value;
   static constexpr int PARTS = TF32 ? 2 : !std::is_same<T, float>::value ? 1 : std::is_same<KVT, __half>::value ? 2 : 3;
+  static constexpr int P_PARTS = PARTS == 1 ? 2 : PARTS;       // of the probabilities
   static constexpr int ROW = D * (int)sizeof(KVT);             // bytes of a key
   static constexpr int KEYS = PR_HALF / ROW;                   // keys of a tile: 16 (8 to 32)
   static constexpr int NT = KEYS / 8;
@@ -281,11 +282,11 @@ __device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t 
     }
   } else {
     constexpr int KS = NT / 2;
-    uint32_t p[KS][4][C::PARTS];
+    uint32_t p[KS][4][C::P_PARTS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) split_pair<Op, C::PARTS>(c[2 * ks + (i >> 1)][(i & 1) * 2], c[2 * ks + (i >> 1)][(i & 1) * 2 + 1], p[ks][i]);
+      for (int i = 0; i < 4; ++i) split_pair<Op, C::P_PARTS>(c[2 * ks + (i >> 1)][(i & 1) * 2], c[2 * ks + (i >> 1)][(i & 1) * 2 + 1], p[ks][i]);
     }
     const int mi = lane >> 3, rr = (mi & 1) * 8 + (lane & 7);
 #pragma unroll
@@ -295,7 +296,7 @@ __device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t 
         uint32_t b0, b1, b2, b3;
         ldmatrix_x4_trans(v_t + pr_part<C::ROW>(ks * 16 + rr, d2 * 2 + (mi >> 1)), b0, b1, b2, b3);
 #pragma unroll
-        for (int part = C::PARTS - 1; part >= 0; --part) {
+        for (int part = C::P_PARTS - 1; part >= 0; --part) {
           Op::mma(A.o[2 * d2], p[ks][0][part], p[ks][1][part], p[ks][2][part], p[ks][3][part], b0, b1);
           Op::mma(A.o[2 * d2 + 1], p[ks][0][part], p[ks][1][part], p[ks][2][part], p[ks][3][part], b2, b3);
         }
@@ -359,10 +360,11 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
     sh.made_end = end;
   };
   if (threadIdx.x == 0) {
-    sh.made = share.find(P, K, sh.line, share.begin);
-    sh.made_end = share.begin + (sh.made.t1 - sh.made.t0);
-    rows_describe(sh.piece[0], sh.made, sh.made_end, K, share);
-    for (int i = 1; i < PR_PIECES; ++i) make_piece(i);
+    const PagedPiece p = sh.line.first;
+    sh.made = p;
+    sh.made_end = share.begin + (p.t1 - p.t0);
+    rows_describe(sh.piece[0], p, sh.made_end, K, share);
+    for (int i = 1; i < PR_PIECES && sh.made_end < share.end; ++i) make_piece(i);
   }
   __syncthreads();
   const uint32_t ring = smem_u32(sc) + warp * PR_STAGES * PR_SLOT, raw_t = smem_u32(sc) + C::RAW, q_t = smem_u32(sc) + C::Q;

@@ -111,7 +111,7 @@ template <typename T, int D>
 cudaError_t chunk_launch(const PagedAttentionParams &P, int min_new, const PagedScratch &S, int blocks, cudaStream_t stream) {
   using C = ChunkTypes<D>;
   const auto kernel = paged_chunk_kernel<T, D>;
-  const PagedCut K{PC_ROWS / (P.nq / P.nkv), PC_LG_TK, min_new, INT32_MAX, 2};
+  const PagedCut K = paged_cut(PC_ROWS / (P.nq / P.nkv), PC_LG_TK, min_new, INT32_MAX, 2);
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(blocks), dim3(PC_THREADS), C::SMEM, stream, P,
                                         chunk_maps(P.pool, P.nkv, D, std::is_same<T, __half>::value), K, S);
@@ -122,7 +122,7 @@ template <typename T, typename KVT, int D>
 cudaError_t attention_launch_t(const PagedAttentionParams &P, int max_new, void *scratch, int n_sms, cudaStream_t stream) {
   using C = RowsTypes<T, KVT, D>;
   const int G = P.nq / P.nkv, blocks = std::min(2 * n_sms, ROWS_BLOCKS);
-  PagedCut K{PR_ROWS / G, C::LG_UNIT, 1, INT32_MAX, PR_LEAST};
+  PagedCut K = paged_cut(PR_ROWS / G, C::LG_UNIT, 1, INT32_MAX, PR_LEAST);
   const PagedScratch S = scratch_at(scratch, 0, ROWS_BLOCKS, PR_ROWS);
   const PagedScratch S_chunk = scratch_at(scratch, scratch_part(ROWS_BLOCKS, PR_ROWS), CHUNK_BLOCKS, PC_ROWS);
   int chunk_blocks = 0;

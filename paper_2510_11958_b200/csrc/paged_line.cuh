@@ -43,6 +43,7 @@ __device__ __forceinline__ long long quotient(long long x, long long y) {
 // Which requests are on a launch's line, and how they are cut.
 struct PagedCut {
   int tile;                          // positions of a row tile
+  int lg_tile;                       // -1: no power of two
   int lg_unit;
   int min_new, max_new;              // requests of that many new rows
   int least;                         // units of a share, at least
@@ -62,8 +63,22 @@ struct PagedRequest {
     const int full = min(m, n / K.tile);
     const int none = c < 0 ? min(full, (int)(-(long long)c / K.tile)) : 0;       // tiles in front of position 0
     long long s = full;
-    if (full > none)
-      s += floor_sum(full - none, 1u << K.lg_unit, K.tile, (long long)c + (long long)(none + 1) * K.tile + (1 << K.lg_unit) - 1);
+    const unsigned n_sum = full - none, lg = K.lg_unit, unit = 1u << lg;
+    const unsigned long long base = (long long)c + (long long)none * K.tile + unit - 1;        // ceil(x / unit) = floor((x + unit - 1) / unit)
+    if (n_sum == 0) {
+    } else if (K.lg_tile < 0) {
+      s += floor_sum(n_sum, unit, K.tile, base + K.tile);
+    } else if (K.lg_tile >= (int)lg) {
+      s += (long long)(base >> lg) * n_sum + ((long long)n_sum * (n_sum + 1) / 2 << (K.lg_tile - lg));
+    } else {
+      // base = q unit + rest: q, and floor(j / r) for the j from rest / tile + 1 on, r = unit / tile
+      const unsigned lr = lg - K.lg_tile, j0 = (unsigned)(base & (unit - 1)) >> K.lg_tile;
+      auto sum_to = [&](unsigned j) {                          // floor(0 / r) + ... + floor(j / r)
+        const long long a = j >> lr;
+        return (a * (a - 1) / 2 << lr) + a * ((j & ((1u << lr) - 1)) + 1);
+      };
+      s += (long long)(base >> lg) * n_sum + sum_to(j0 + n_sum) - sum_to(j0);
+    }
     return m > full ? s + units(K, full) : s;
   }
 };
@@ -218,6 +233,10 @@ struct PagedCutItem {
   int b, row0, rows, first_seen, kvh;     // request, first row of q, rows, keys that the first row sees
   int pad[2];
 };
+
+inline PagedCut paged_cut(int tile, int lg_unit, int min_new, int max_new, int least) {
+  return PagedCut{tile, (tile & (tile - 1)) ? -1 : 31 - __builtin_clz((unsigned)tile), lg_unit, min_new, max_new, least};
+}
 
 // Scratch: an entry per block, then two partial results per block: [tile rows][D] floats (the chunk kernel: [D / 4][tile
 // rows][4]) and (level, sum) per row.

@@ -298,16 +298,18 @@ dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32
  *                             16-byte aligned, owned by the caller; holds partial results while the call's
  *                             kernels run (calls sharing one scratch must be stream-ordered, captured
  *                             graphs among them).  Nothing in it needs to be cleared or kept
- *   out [n_rows][n_q_heads][head_dim]   in q_dtype.  Rows of no request are left as they were
- * Types: fp32 queries with any cache (results to fp32 accuracy: fp32 queries, and probabilities, enter
- * the tensor cores as two or three 16-bit parts), or 16-bit queries with a cache of the same type (the probabilities
- * are rounded once to that type before the product with V, sums and maxima are fp32).  A row that sees no key (a length below
+ *   out [n_rows][n_q_heads][head_dim]   in q_dtype; overlaps no other array.  Rows of no request
+ *                             are left as they were
+ * Types: fp32 queries with any cache (results to fp32 accuracy: queries and probabilities enter
+ * the tensor cores in two or three parts), or 16-bit queries with a cache of the same type (requests with
+ * more than 64 query rows to a kv head: the probabilities are rounded once to that type before the product
+ * with V; others: in two parts).  Sums and maxima are fp32.  A row that sees no key (a length below
  * its rows, pages outside the pool, which take their keys out), or none whose weight is not zero, gives zeros.
  * Keys and values of positions that a row does not see have no influence on it, whatever they hold.
  * Errors: SHAPE for head_dim not 64/128, n_q_heads % n_kv_heads != 0 or more than 16 query heads per
  * KV head; UNSUPPORTED for 16-bit queries and a cache of another type; INVALID_ARG for rows that do
  * not begin on 16-byte boundaries or strides shorter than a row; CAPACITY if scratch_bytes is too small, or
- * beyond DMTD_PAGED_MAX_REQUESTS requests, 2^31 - 1 positions to a table row, 2^24 query rows times heads. */
+ * beyond DMTD_PAGED_MAX_REQUESTS requests, 2^30 positions to a table row, 2^24 query rows times heads. */
 #define DMTD_PAGED_ATTENTION_SCRATCH_BYTES (48u << 20)
 dmtd_status dmtd_paged_attention(const void *q, int32_t q_dtype, int64_t q_stride, int32_t n_rows,
                                  int32_t n_q_heads, const int32_t *row_start, const int32_t *lens,

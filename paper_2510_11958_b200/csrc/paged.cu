@@ -245,8 +245,8 @@ dmtd_status dmtd_paged_attention(const void *q, int32_t q_dtype, int64_t q_strid
     return call_failed(DMTD_ERR_SHAPE, "paged_attention: n_q_heads must be a multiple of n_kv_heads, at most 16 per kv head");
   if ((int64_t)n_rows * n_q_heads > INT32_MAX / 128) return call_failed(DMTD_ERR_CAPACITY, "paged_attention: more than 2^24 query rows and heads");
   if (n_requests > DMTD_PAGED_MAX_REQUESTS) return call_failed(DMTD_ERR_CAPACITY, "paged_attention: more than %d requests", DMTD_PAGED_MAX_REQUESTS);
-  if (((int64_t)table_stride << P.pool.lg_page) > INT32_MAX)
-    return call_failed(DMTD_ERR_CAPACITY, "paged_attention: a table row names more than 2^31 - 1 positions");
+  if (((int64_t)table_stride << P.pool.lg_page) > 1 << 30)
+    return call_failed(DMTD_ERR_CAPACITY, "paged_attention: a table row names more than 2^30 positions");
   if (n_rows == 0 || n_requests == 0) return DMTD_OK;
   if (!q || !out || !row_start || !lens || !table || !scratch) return call_failed(DMTD_ERR_INVALID_ARG, "paged_attention: null pointer");
   if (scratch_bytes < DMTD_PAGED_ATTENTION_SCRATCH_BYTES)

@@ -222,6 +222,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       }
     } else if (warp == 10) {
       // ---- copies: K and V tiles in turn through the ring
+      fence_proxy_async_global();                              // the cache's new rows were written by ordinary stores
       constexpr int PARTS = D / 8;
       const int rows_here = min(1 << lg, PC_TK);               // of a tile, in one page
       const int n_pages = PC_TK / rows_here;                   // pages of a tile

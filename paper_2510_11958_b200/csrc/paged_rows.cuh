@@ -49,6 +49,7 @@ struct RowsShared {
   PagedPiece made;                   // the last piece made, by thread 0
   long long made_end;                // ... its end on the line
   RowsPiece piece[PR_PIECES];
+  float size[16];                              // powers of two of the query rows (RowsTypes::SIZED)
   uint32_t there[PR_WARPS][PR_STAGES];         // a bit per key of a ring slot
 };
 
@@ -75,6 +76,8 @@ struct RowsTypes {
   static constexpr int Q = OS;
   static constexpr int RED = OS + PR_WARPS * PR_ROWS * OROW * 4;
   static constexpr int SMEM = RED + 2 * PR_WARPS * PR_ROWS * 4;
+  // fp32 queries in fp16 parts: a row is brought to the size of 1 by a power of two, which its scores are multiplied with
+  static constexpr bool SIZED = PARTS == 2 && !TF32;
   static_assert(Q_PARTS * PR_ROWS * QROW <= RED - OS, "parts of the queries");
   static_assert(2 * (SMEM + 1024 + (int)sizeof(RowsShared)) <= 228 * 1024, "two blocks per SM");
 };
@@ -134,7 +137,7 @@ struct RowsAcc {
 // A warp's tile of keys against the 16 query rows.  q_t: the queries in shared memory; qh: what of them is in registers.
 // lim[h]: keys that row g + 8 h sees, counted from the tile's first; good: a bit per key that is there at all.
 template <class C, typename KVT, int D, class QRegs>
-__device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t v_t, uint32_t q_t, const QRegs &qh, float scale,
+__device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t v_t, uint32_t q_t, const QRegs &qh, const float (&scale)[2],
                                           const int (&lim)[2], uint32_t good, bool mask) {
   using Op = typename std::conditional<std::is_same<KVT, __half>::value, OpF16, OpBf16>::type;
   constexpr int NT = C::NT;
@@ -170,7 +173,7 @@ __device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t 
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) c[j][e] = (c[j][e] + lo[j][e]) * scale;
+      for (int e = 0; e < 4; ++e) c[j][e] = (c[j][e] + lo[j][e]) * scale[e >> 1];
     }
   } else {
     float c2[NT][4];
@@ -206,7 +209,7 @@ __device__ __forceinline__ void rows_tile(RowsAcc<D> &A, uint32_t k_t, uint32_t 
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) c[j][e] = (c[j][e] + c2[j][e]) * scale;
+      for (int e = 0; e < 4; ++e) c[j][e] = (c[j][e] + c2[j][e]) * scale[e >> 1];
     }
   }
   if (mask) {
@@ -518,11 +521,24 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
       for (int k = 0; k < PR_ROWS * D / 8 / PR_THREADS; ++k) {
         const int idx = threadIdx.x + k * PR_THREADS, qi = idx / (D / 8), at = idx % (D / 8);
         const uint4 x = lds128(raw_t + qi * C::RAW_ROW + at * 32), y = lds128(raw_t + qi * C::RAW_ROW + at * 32 + 16);
+        float f[8] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w),
+                      __uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)};
+        if constexpr (C::SIZED) {
+          float most = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(f[j]));
+#pragma unroll
+          for (int o = 1; o < D / 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+          // the exponent of the largest, kept where 2^+-exponent is a normal number (0, infinities: any)
+          const int exponent = min(max((int)(__float_as_uint(most) >> 23) - 127, -100), 100);
+          const float down = __uint_as_float((uint32_t)(127 - exponent) << 23);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] *= down;
+          if (at == 0) sh.size[qi] = __uint_as_float((uint32_t)(127 + exponent) << 23);
+        }
         uint32_t w[4][C::PARTS];
-        split_pair<Op, C::PARTS>(__uint_as_float(x.x), __uint_as_float(x.y), w[0]);
-        split_pair<Op, C::PARTS>(__uint_as_float(x.z), __uint_as_float(x.w), w[1]);
-        split_pair<Op, C::PARTS>(__uint_as_float(y.x), __uint_as_float(y.y), w[2]);
-        split_pair<Op, C::PARTS>(__uint_as_float(y.z), __uint_as_float(y.w), w[3]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) split_pair<Op, C::PARTS>(f[2 * j], f[2 * j + 1], w[j]);
 #pragma unroll
         for (int part = 0; part < C::PARTS; ++part)
           sts128(q_t + (part * PR_ROWS + qi) * C::QROW + at * 16, make_uint4(w[0][part], w[1][part], w[2][part], w[3][part]));
@@ -536,6 +552,7 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
     // ---- keys
     RowsAcc<D> A;
     A.clear();
+    const float row_scale[2] = {C::SIZED ? scale * sh.size[g] : scale, C::SIZED ? scale * sh.size[g + 8] : scale};
     const int lim0[2] = {min(d.keys, d.pos + (int)(g * g_inv >> 16) + 1), min(d.keys, d.pos + (int)((g + 8) * g_inv >> 16) + 1)};
 #pragma unroll 1
     for (int i = d.u0; i < d.u1; ++i) {
@@ -546,7 +563,7 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
       if (key0 < d.keys) {
         const uint32_t good = sh.there[warp][slot];
         const int lim[2] = {lim0[0] - key0, lim0[1] - key0};
-        rows_tile<C, KVT, D>(A, k_t, k_t + PR_HALF, q_t, qh, scale, lim, good,
+        rows_tile<C, KVT, D>(A, k_t, k_t + PR_HALF, q_t, qh, row_scale, lim, good,
                              key0 + C::KEYS > d.pos + 1 || good != (C::KEYS == 32 ? 0xffffffffu : (1u << C::KEYS) - 1));
       }
       __syncwarp();                                            // the slot is free

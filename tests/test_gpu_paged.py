@@ -378,6 +378,50 @@ def test_scores_far_apart(pkg, qt, kv):
     check_attention(pkg, c)
 
 
+@pytest.mark.parametrize("kv", [F32, BF16, F16])
+@pytest.mark.parametrize("size", [1e-30, 1e-6, 1e4, 3e5])
+def test_queries_of_any_size(pkg, kv, size):
+    """fp32 queries far outside fp16's range (and its precision): scores stay moderate through small or large keys."""
+    new = 9
+    c = attention_case(11, [200], [new], 8, 2, 64, F32, kv, 16, "hnd")
+    c["q"] *= size / 1.5
+    c["q"][4:, :, 5:] = 0.0
+    if size > 1:
+        c["kc"][:] = (c["kc"].float() * min(1.0, 4.0 / size)).to(kv)
+    ref, spread = attention_reference(c["q"], c["start"], c["lens"], c["table"], c["kc"], c["vc"], c["out"])
+    got = pkg.paged_attention(c["q"], ints(c["start"]), ints(c["lens"]), c["table"], c["kc"], c["vc"])
+    # (no further than the other tests: the parts are relative to the row's largest value)
+    assert ((got.double() - ref).abs() <= 2e-5 * spread + 1e-5).all()
+
+
+@pytest.mark.parametrize("qt,kv", [(F32, F16), (BF16, BF16)])
+@pytest.mark.parametrize("B", [257, 700])
+def test_more_requests_than_are_kept(pkg, qt, kv, B):
+    """Batches whose requests do not fit shared memory; pieces of prompts far behind the first requests."""
+    rng = random.Random(B)
+    cached = [rng.choice([0, rng.randint(0, 30), rng.randint(0, 200)]) for _ in range(B)]
+    new = [rng.choice([0, 1, 1, 2]) for _ in range(B)]
+    for b in (B - 1, B // 2, 70):
+        new[b] = 90
+    c = attention_case(12, cached, new, 4, 2, 64, qt, kv, 16, "hnd", pad=1)
+    check_attention(pkg, c)
+
+
+def test_tables_of_the_largest_kind(pkg):
+    """A request near the end of the plan's and the attention's ranges: positions around 2^20 in a sparse table."""
+    page, n = 1024, 1 << 20
+    kc, vc = pool(3, 1, page, 64, BF16, "hnd")
+    g = torch.Generator(device="cuda").manual_seed(13)
+    for t in (kc, vc):
+        t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+    table = torch.full((1, n // page), -1, dtype=torch.int32, device="cuda")
+    table[0, 0], table[0, 700], table[0, -1] = 2, 0, 1               # all others have been dropped
+    for new in (1, 200):
+        q = torch.randn(new, 2, 64, generator=g, device="cuda").to(BF16)
+        c = dict(q=q, start=[0, new], lens=[n], table=table, kc=kc, vc=vc, out=torch.zeros_like(q))
+        check_attention(pkg, c)
+
+
 @pytest.mark.parametrize("kv", [BF16, F32])
 def test_offsets_beyond_32_bits(pkg, kv):
     """A pool of more than 2^32 bytes and 2^31 values, keys at both ends."""

@@ -301,9 +301,9 @@ dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32
  *   out [n_rows][n_q_heads][head_dim]   in q_dtype; overlaps no other array.  Rows of no request
  *                             are left as they were
  * Types: fp32 queries with any cache (results to fp32 accuracy: queries and probabilities enter
- * the tensor cores in two or three parts), or 16-bit queries with a cache of the same type (requests with
- * more than 64 query rows to a kv head: the probabilities are rounded once to that type before the product
- * with V; others: in two parts).  Sums and maxima are fp32.  A row that sees no key (a length below
+ * the tensor cores in two or three parts), or 16-bit queries with a cache of the same type (in requests
+ * with some dozens of query rows to a kv head the probabilities are rounded once to that type before the
+ * product with V, in others they enter it in two parts).  Sums and maxima are fp32.  A row that sees no key (a length below
  * its rows, pages outside the pool, which take their keys out), or none whose weight is not zero, gives zeros.
  * Keys and values of positions that a row does not see have no influence on it, whatever they hold.
  * Errors: SHAPE for head_dim not 64/128, n_q_heads % n_kv_heads != 0 or more than 16 query heads per

@@ -104,8 +104,11 @@ ChunkMaps chunk_maps(const PagedPool &pool, int nkv, int D, bool f16) {
   return m;
 }
 
-// Requests with at least this many query rows to a kv head go to the chunk kernel.
-constexpr int CHUNK_LEAST_ROWS = 65;
+// Requests with at least this many query rows to a kv head go to the chunk kernel, which takes the same time for 16 and for
+// 128 of them; the row kernel reads the keys anew for every 16.  us, chunk / row kernel, bf16, head_dim 128, 8 kv heads: 8 requests x
+// 4000 keys 48 / 42 with 32 rows, 49 / 57 with 48; 32 x 1000 keys 52 / 48 and 53 / 63; one request x 1000 keys 19 / 13 and 20 / 14 (the
+// lengths are not known here).  head_dim 64: 8 x 4000 keys 41 / 40 with 48 rows, 41 / 50 with 64.
+constexpr int chunk_least_rows(int D) { return D == 128 ? 33 : 49; }
 
 template <typename T, int D>
 cudaError_t chunk_launch(const PagedAttentionParams &P, int min_new, const PagedScratch &S, int blocks, cudaStream_t stream) {
@@ -128,7 +131,7 @@ cudaError_t attention_launch_t(const PagedAttentionParams &P, int max_new, void 
   int chunk_blocks = 0;
   cudaError_t e = cudaSuccess;
   if constexpr (std::is_same<T, KVT>::value && !std::is_same<T, float>::value) {
-    const int min_new = (CHUNK_LEAST_ROWS + G - 1) / G;
+    const int min_new = (chunk_least_rows(D) + G - 1) / G;
     if (max_new >= min_new) {
       chunk_blocks = std::min(n_sms, CHUNK_BLOCKS);
       e = chunk_launch<T, D>(P, min_new, S_chunk, chunk_blocks, stream);

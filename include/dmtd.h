@@ -252,7 +252,8 @@ typedef struct {
  *   n_free_out [1]            entries left on the stack.  May be n_free
  * Pages are given out in the order of requests.  A request is refused as a whole, and keeps what it
  * has, if the stack does not hold all the pages that it and those in front of it ask for, if it would outgrow
- * its table row, or if its rows do not end within n_rows.  Its rows keep their place.
+ * its table row, or if its rows do not end within n_rows.  Its rows keep their place (dmtd_paged_append
+ * passes them over; what dmtd_paged_attention gives for them means nothing).
  * The arrays that are written must not overlap others but where it says so above.
  * Errors: SHAPE if page_size is not a power of two; CAPACITY for more than DMTD_PAGED_MAX_REQUESTS
  * requests, 2^31 - 1 slots, or 2^30 rows or table entries. */
@@ -269,7 +270,7 @@ dmtd_status dmtd_paged_plan(const int32_t *lens, const int32_t *n_new, int32_t n
  *   q [n_rows][n_q_heads][head_dim], k, v [n_rows][n_kv_heads][head_dim]   in `dtype`, rows
  *                             q_stride / k_stride / v_stride values apart (three parts of one
  *                             projection's output, say), heads dense
- *   q_norm, k_norm            float [head_dim], or NULL: no norm
+ *   q_norm, k_norm            float [head_dim], 16-byte aligned, or NULL: no norm
  *   rope_theta                0: no rotation
  *   position, slot [n_rows]   rows whose slot is outside the pool are left alone, in the
  *                             cache and in q_out.  Slots of a call are distinct: two rows with the

@@ -210,6 +210,7 @@ dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32
     return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: a row stride is shorter than a row");
   if (!aligned16(k) || !aligned16(v) || k_stride % unit || v_stride % unit || (n_q_heads && (!aligned16(q) || !aligned16(q_out) || q_stride % unit)))
     return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: rows must begin on 16-byte boundaries");
+  if (!aligned16(q_norm) || !aligned16(k_norm)) return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: norms must begin on 16-byte boundaries");
   P.q = q; P.k = k; P.v = v;
   P.q_stride = q_stride; P.k_stride = k_stride; P.v_stride = v_stride;
   P.n_rows = n_rows; P.nq = n_q_heads; P.nkv = nkv;

@@ -74,7 +74,7 @@ def test_cache_refusals(dll, want, kw):
     ("INVALID_ARG", dict(n_rows=-1)), ("SHAPE", dict(dtype=7)), ("INVALID_ARG", dict(q=None)), ("INVALID_ARG", dict(slot=None)),
     ("INVALID_ARG", dict(q_out=None)), ("INVALID_ARG", dict(theta=-1.0)), ("INVALID_ARG", dict(theta=float("nan"))),
     ("INVALID_ARG", dict(theta=float("inf"))), ("INVALID_ARG", dict(eps=-1.0)), ("INVALID_ARG", dict(q_stride=1000)),
-    ("INVALID_ARG", dict(k_stride=258)), ("INVALID_ARG", dict(v=A + 4)),
+    ("INVALID_ARG", dict(k_stride=258)), ("INVALID_ARG", dict(v=A + 4)), ("INVALID_ARG", dict(q_norm=A + 4)), ("INVALID_ARG", dict(k_norm=A + 8)),
 ])
 def test_append_refusals(dll, want, kw):
     assert _append(dll, **kw) == STATUS[want]

@@ -6,4 +6,4 @@ library; creating a `Dmtd` does, and fails loudly if the library has not been bu
 CUDA device is present.  There is no CPU fallback.
 """
 from .binding import Dmtd, DmtdError, load_library, library_path, declared_symbols, attention_decode, attention_decode_static, PagedPlan, \
-    paged_plan, paged_append, paged_attention  # noqa: F401
+    paged_plan, paged_append, paged_attention, PAGED_ATTENTION_SCRATCH_BYTES  # noqa: F401

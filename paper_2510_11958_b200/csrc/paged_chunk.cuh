@@ -568,7 +568,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         // rows that are not finite: see the row kernel
-        if (ok && c.rows > 1) {
+        if (ok) {
           uint32_t bad_rows = __ballot_sync(0xffffffffu, !good);
           __syncwarp();
           while (bad_rows) {

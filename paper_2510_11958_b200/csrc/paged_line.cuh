@@ -299,7 +299,7 @@ __device__ __forceinline__ void paged_join_row(const PagedAttentionParams &P, co
     good = good && isfinite(o[e]);
   }
   const int r = qi / G, row = c.row0 + r, head = c.kvh * G + qi - r * G;
-  if (c.rows > 1 && !__all_sync(0xffffffffu, good)) paged_attend_row<T, KVT, D>(P, c.b, row, c.first_seen + r, head);
+  if (!__all_sync(0xffffffffu, good)) paged_attend_row<T, KVT, D>(P, c.b, row, c.first_seen + r, head);
   else store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o);
 }
 
@@ -337,7 +337,7 @@ __device__ __forceinline__ void paged_join_rows(const PagedAttentionParams &P, c
 #pragma unroll
     for (int k = 0; k < 2; ++k) store_pack(dst + 8 * k, *reinterpret_cast<float(*)[8]>(o + 8 * k));
   }
-  uint32_t bad_rows = __ballot_sync(0xffffffffu, mine && !good && c.rows > 1);
+  uint32_t bad_rows = __ballot_sync(0xffffffffu, mine && !good);
   __syncwarp();
   while (bad_rows) {
     const int i = q0 + __ffs(bad_rows) - 1, r = i / G;

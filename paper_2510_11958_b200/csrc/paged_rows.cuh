@@ -626,8 +626,8 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
       }
     }
     // A row that is not finite: a probability of zero may have met an infinity or a NaN in a row of V that it does not see
-    // (a later one of the same tile).  Such tiles are worked out again row by row.
-    if (d.rows > 1 && __syncthreads_or(!good)) {
+    // (a later one of the same tile), or the second part of a value an infinity.  Such tiles are worked out again row by row.
+    if (__syncthreads_or(!good)) {
       for (int qi = warp; qi < nQ; qi += PR_WARPS) {
         const int r = qi * g_inv >> 16;
         paged_attend_row<T, KVT, D>(P, d.b, d.row0 + r, d.pos + r + 1, d.kvh * G + qi - r * G);

@@ -368,6 +368,22 @@ def test_values_that_a_row_does_not_see(pkg, qt, kv, new):
 
 
 @pytest.mark.parametrize("qt,kv", TYPES)
+@pytest.mark.parametrize("cached,new", [([200, 900, 17], [1, 1, 1]), ([100, 3000, 40], [2, 1, 40])])
+def test_infinities_in_sight(pkg, qt, kv, cached, new):
+    """An infinite value gives infinite results, a score of minus infinity takes its key out: in tiles of one row as in others."""
+    c = attention_case(14, cached, new, 8, 2, 128, qt, kv, 16, "hnd")
+    c["q"][:, :, 0] = c["q"][:, :, 0].abs() + 0.25
+    for b in range(3):
+        page = c["table"][b, 0].long()
+        c["vc"][page, :, 5, 3:60] = math.inf
+        c["vc"][page, :, 5, 60:70] = -math.inf
+        c["kc"][page, :, 9, 0] = -math.inf
+    got = check_attention(pkg, c, finite=False)
+    assert (got[:, :, 3:60] == math.inf).all() and (got[:, :, 60:70] == -math.inf).all()
+    assert torch.isfinite(got[:, :, :3]).all() and torch.isfinite(got[:, :, 70:]).all()
+
+
+@pytest.mark.parametrize("qt,kv", TYPES)
 def test_scores_far_apart(pkg, qt, kv):
     """One key outweighs all others by far, early or late; equal scores; large ones."""
     c = attention_case(5, [300, 300, 300, 0], [1, 4, 20, 64], 8, 2, 64, qt, kv, 16, "nhd", scale=1.0)

@@ -278,7 +278,7 @@ dmtd_status dmtd_paged_plan(const int32_t *lens, const int32_t *n_new, int32_t n
  *   q_out [n_rows][n_q_heads][head_dim]   in `dtype`; may be q where q is dense
  * n_q_heads may be 0 (keys and values only).  Arithmetic is fp32 (angles: 64 bits), each result is rounded once.
  * Errors: INVALID_ARG for rows that do not begin on 16-byte boundaries or strides shorter than a
- * row; SHAPE for types and head_dim. */
+ * row; SHAPE for types and head_dim; CAPACITY for more than 2^16 heads. */
 dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32_t dtype,
                               int64_t q_stride, int64_t k_stride, int64_t v_stride, int32_t n_rows,
                               int32_t n_q_heads, const float *q_norm, const float *k_norm,

@@ -204,12 +204,15 @@ dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32
   if (n_rows == 0) return DMTD_OK;
   if (!k || !v || !position || !slot || (n_q_heads && (!q || !q_out))) return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: null pointer");
   const int D = cache->head_dim, nkv = cache->n_kv_heads;
+  if (n_q_heads > 65536 || nkv > 65536) return call_failed(DMTD_ERR_CAPACITY, "paged_append: more than 2^16 heads");
   const int64_t unit = 16 / dtype_bytes(dtype);
   if (n_rows == 1) q_stride = k_stride = v_stride = 0;
   else if ((n_q_heads && q_stride < (int64_t)n_q_heads * D) || k_stride < (int64_t)nkv * D || v_stride < (int64_t)nkv * D)
     return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: a row stride is shorter than a row");
   if (!aligned16(k) || !aligned16(v) || k_stride % unit || v_stride % unit || (n_q_heads && (!aligned16(q) || !aligned16(q_out) || q_stride % unit)))
     return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: rows must begin on 16-byte boundaries");
+  if (q_out == q && n_q_heads && n_rows > 1 && q_stride != (int64_t)n_q_heads * D)
+    return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: q_out may be q only where q is dense");
   if (!aligned16(q_norm) || !aligned16(k_norm)) return call_failed(DMTD_ERR_INVALID_ARG, "paged_append: norms must begin on 16-byte boundaries");
   P.q = q; P.k = k; P.v = v;
   P.q_stride = q_stride; P.k_stride = k_stride; P.v_stride = v_stride;
@@ -260,6 +263,7 @@ dmtd_status dmtd_paged_attention(const void *q, int32_t q_dtype, int64_t q_strid
   else if (q_stride < (int64_t)n_q_heads * D) return call_failed(DMTD_ERR_INVALID_ARG, "paged_attention: the row stride is shorter than a row");
   if (!aligned16(q) || !aligned16(out) || !aligned16(scratch) || q_stride % (16 / (int64_t)dtype_bytes(q_dtype)))
     return call_failed(DMTD_ERR_INVALID_ARG, "paged_attention: rows and scratch must begin on 16-byte boundaries");
+  if (out == q) return call_failed(DMTD_ERR_INVALID_ARG, "paged_attention: out must not be q");
   P.q = q; P.q_stride = q_stride; P.out = out;
   P.batch = PagedBatch{row_start, lens, table, n_requests, table_stride, n_rows};
   P.nq = n_q_heads; P.nkv = nkv;

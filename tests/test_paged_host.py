@@ -39,7 +39,7 @@ def _append(dll, cache=None, **kw):
 
 def _attention(dll, cache=None, **kw):
     a = dict(q=A, q_dtype=1, q_stride=1024, n_rows=8, nq=8, row_start=A, lens=A, n_requests=4, table=A, table_stride=10, max_new=0,
-             cache=cache or _cache(), scratch=A, scratch_bytes=PAGED_ATTENTION_SCRATCH_BYTES, out=A, stream=None)
+             cache=cache or _cache(), scratch=A, scratch_bytes=PAGED_ATTENTION_SCRATCH_BYTES, out=2 * A, stream=None)
     a.update(kw)
     return dll.dmtd_paged_attention(*a.values())
 
@@ -75,6 +75,7 @@ def test_cache_refusals(dll, want, kw):
     ("INVALID_ARG", dict(q_out=None)), ("INVALID_ARG", dict(theta=-1.0)), ("INVALID_ARG", dict(theta=float("nan"))),
     ("INVALID_ARG", dict(theta=float("inf"))), ("INVALID_ARG", dict(eps=-1.0)), ("INVALID_ARG", dict(q_stride=1000)),
     ("INVALID_ARG", dict(k_stride=258)), ("INVALID_ARG", dict(v=A + 4)), ("INVALID_ARG", dict(q_norm=A + 4)), ("INVALID_ARG", dict(k_norm=A + 8)),
+    ("INVALID_ARG", dict(q_stride=1032)), ("CAPACITY", dict(nq=65537)),
 ])
 def test_append_refusals(dll, want, kw):
     assert _append(dll, **kw) == STATUS[want]
@@ -87,6 +88,7 @@ def test_append_refusals(dll, want, kw):
     ("CAPACITY", dict(n_rows=1 << 22)), ("CAPACITY", dict(table_stride=1 << 27)), ("CAPACITY", dict(scratch_bytes=PAGED_ATTENTION_SCRATCH_BYTES - 1)),
     ("INVALID_ARG", dict(scratch=None)), ("INVALID_ARG", dict(out=None)), ("INVALID_ARG", dict(lens=None)), ("INVALID_ARG", dict(q_stride=1016)),
     ("INVALID_ARG", dict(q_stride=1028)), ("INVALID_ARG", dict(q=A + 2)), ("INVALID_ARG", dict(out=A + 8)), ("INVALID_ARG", dict(scratch=A + 4)),
+    ("INVALID_ARG", dict(out=A)),
 ])
 def test_attention_refusals(dll, want, kw):
     assert _attention(dll, **kw) == STATUS[want]

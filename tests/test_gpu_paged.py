@@ -551,6 +551,56 @@ def test_on_another_stream(pkg):
     assert torch.equal(got, want)
 
 
+def _three_cases():
+    return [attention_case(15, [900, 4], [200, 1], 8, 2, 128, BF16, BF16, 16, "hnd"), attention_case(16, [2500, 80, 7], [1, 3, 2], 16, 2, 64, F32, F16, 4, "nhd"),
+            attention_case(17, [0, 1300, 60], [90, 1, 40], 8, 8, 64, F16, F16, 32, "mix")]
+
+
+def _args(c):
+    return c["q"], ints(c["start"]), ints(c["lens"]), c["table"], c["kc"], c["vc"]
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_calls_in_a_row_share_scratch(pkg, graph):
+    """Each call's first kernel starts under the last one's end: partial results of the call in front must be read by then."""
+    cases = _three_cases()
+    args, want = [_args(c) for c in cases], [check_attention(pkg, c) for c in cases]
+    scratch = torch.empty(pkg.PAGED_ATTENTION_SCRATCH_BYTES, dtype=torch.uint8, device="cuda")
+    order = [random.Random(1).randrange(3) for _ in range(40)]
+    outs = [cases[i]["out"].clone() for i in order]
+
+    def calls():
+        for i, out in zip(order, outs):
+            pkg.paged_attention(*args[i], scratch=scratch, out=out)
+    if graph:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            calls()
+        for _ in range(3):
+            g.replay()
+    else:
+        calls()
+    for i, out in zip(order, outs):
+        assert torch.equal(out, want[i])
+
+
+def test_two_streams_at_once(pkg):
+    """Calls with scratch of their own run side by side."""
+    cases = _three_cases()
+    args, want = [_args(c) for c in cases], [check_attention(pkg, c) for c in cases]
+    outs = [[c["out"].clone() for _ in range(30)] for c in cases]
+    scratch = [torch.empty(pkg.PAGED_ATTENTION_SCRATCH_BYTES, dtype=torch.uint8, device="cuda") for _ in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for n in range(30):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                pkg.paged_attention(*args[i], scratch=scratch[i], out=outs[i][n])
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert all(torch.equal(x, w) for x in o)
+
+
 def test_against_the_contiguous_cache(pkg):
     """Equal lengths: what dmtd_attention_decode gives for the same keys in one piece."""
     B, R, nq, nkv, D, n, page = 3, 3, 8, 2, 128, 400, 16

@@ -75,7 +75,9 @@ PagedScratch scratch_at(void *scratch, size_t offset, int blocks, int rows) {
   return PagedScratch{items, reinterpret_cast<float *>(items + blocks), rows};
 }
 
-// The pool as TMA sees it: [page][kv head][row][D], 64 dimensions of up to 128 rows of a page to a copy.
+// The pool as TMA sees it: [page and kv head][groups of 8 rows][64 dimensions][8 rows][64 values of them], up to 32 rows of a page with
+// all their dimensions to a copy (a copy takes its SM some 100 cycles and more whatever its size: two of 64 dimensions each for
+// pages of 16 rows were the bound of the chunk kernel, 236 us for 2000 rows over 8000 keys).
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeTiled encode_tiled() {
@@ -89,15 +91,21 @@ EncodeTiled encode_tiled() {
 }
 ChunkMaps chunk_maps(const PagedPool &pool, int nkv, int D, bool f16) {
   ChunkMaps m{};
+  // page and head are one axis: pages are a whole number of heads apart
   if (pool.lg_page < 3 || !encode_tiled()) return m;
-  const cuuint64_t dims[4] = {(cuuint64_t)D, 1ull << pool.lg_page, (cuuint64_t)nkv, (cuuint64_t)pool.n_pages};
-  auto bytes = [&](long long stride) { return (cuuint64_t)(stride ? stride : D) * 2; };           // (of an axis of one: anything)
-  const cuuint64_t strides[3] = {bytes(pool.row_stride), bytes(pool.head_stride), bytes(pool.page_stride)};
-  const cuuint32_t box[4] = {64, (cuuint32_t)std::min(1 << pool.lg_page, PC_TK), 1, 1}, step[4] = {1, 1, 1, 1};
+  const long long head = nkv > 1 ? pool.head_stride : pool.n_pages > 1 ? pool.page_stride : D;
+  const long long apart = pool.n_pages > 1 ? pool.page_stride / head : 1, cells = (pool.n_pages - 1) * apart + nkv;
+  if ((pool.n_pages > 1 && pool.page_stride % head) || cells > INT32_MAX) return m;
+  const cuuint64_t row = pool.row_stride * 2;
+  const cuuint64_t dims[5] = {64, 8, (cuuint64_t)D / 64, 1ull << (pool.lg_page - 3), (cuuint64_t)cells};
+  const cuuint64_t strides[4] = {row, 128, 8 * row, (cuuint64_t)head * 2};
+  const cuuint32_t box[5] = {64, 8, (cuuint32_t)D / 64, (cuuint32_t)std::min(1 << pool.lg_page, PC_BOX) / 8, 1}, step[5] = {1, 1, 1, 1, 1};
   const void *base[2] = {pool.k, pool.v};
   m.on = 1;
+  m.apart = (int)apart;
+  m.cells = (int)cells;
   for (int i = 0; i < 2; ++i)
-    if (encode_tiled()(&m.map[i], f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base[i]), dims, strides, box,
+    if (encode_tiled()(&m.map[i], f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base[i]), dims, strides, box,
                        step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       m.on = 0;                                          // (strides that TMA cannot hold: 16-byte copies)

@@ -11,8 +11,8 @@
 // As in the row kernel a row's reference is raised only when a score lies more than 2^6 above it; then O is read
 // back and scaled.
 //
-// K and V tiles (rows of 64 values with the 128-byte swizzle, as K-major operand of S and as N-major operand of P V) come
-// through one ring, in turn, a TMA copy to a page and 64 dimensions; page ids are looked up a tile ahead.  Pages that are not there are
+// K and V tiles (atoms of 8 rows of 64 values with the 128-byte swizzle, as K-major operand of S and as N-major operand of P V) come
+// through one ring, in turn, a TMA copy to a page or 32 of its rows; page ids are looked up a tile ahead.  Pages that are not there are
 // copied from behind the pool's end, which fills zeros; the page that holds the last key, whose rows behind it may hold anything,
 // comes by 16-byte copies that fill zeros (0 times a stale NaN would not be 0), and so does everything in pools whose pages have fewer than 8
 // positions (a swizzle atom).  (All copies 16 bytes wide, by two warps: 885 us for 2000 rows over 8000 keys, where the tensor cores
@@ -34,7 +34,7 @@ constexpr int PC_TK = 128, PC_LG_TK = 7;                       // keys of a tile
 constexpr int PC_STEP = 64;                                    // keys of a step
 constexpr int PC_THREADS = 384;
 constexpr int PC_PIECES = 3;
-constexpr int PC_HALF = 128 * 128;                             // bytes of 64 dimensions of 128 rows
+constexpr int PC_BOX = 32;                                     // rows of a copy, at most
 constexpr float PC_ABOVE = 6.f;
 constexpr int PC_TMEM = 512;                                   // two S (P over them) and O of both halves
 constexpr long long PC_WAIT_TICKS = 2000000000ll;              // about a second
@@ -85,8 +85,7 @@ struct ChunkShared {
 
 template <int D>
 struct ChunkTypes {
-  static constexpr int PANELS = D / 64;                        // 128-byte wide columns of a tile
-  static constexpr int TILE = PANELS * PC_HALF;
+  static constexpr int TILE = PC_TK * D * 2;
   static constexpr int Q = 0;
   static constexpr int RING = 2 * TILE;
   static constexpr int STAGES = D == 128 ? 5 : 8;
@@ -94,11 +93,13 @@ struct ChunkTypes {
   static_assert(SMEM + (int)sizeof(ChunkShared) <= 227 * 1024 - 16, "shared memory");
 };
 
-// byte offset of 16-byte part `part` of row `row` in a tile
+// A tile: swizzle atoms of 8 rows x 64 dimensions, [row / 8][dimension / 64].  Byte offset of 16-byte part `part` of row `row`
+template <int D>
 __device__ __forceinline__ uint32_t pc_part(int row, int part) {
-  return (uint32_t)((part >> 3) * PC_HALF + row * 128 + (((part & 7) ^ (row & 7)) << 4));
+  return (uint32_t)((row >> 3) * (D * 16) + (part >> 3) * 1024 + (row & 7) * 128 + (((part & 7) ^ (row & 7)) << 4));
 }
-__device__ __forceinline__ uint64_t pc_desc(uint32_t addr, uint32_t lbo) { return umma_smem_desc(addr, lbo, 1024) | (2ull << 61); }
+template <int D>
+__device__ __forceinline__ uint64_t pc_desc(uint32_t addr, uint32_t lbo) { return umma_smem_desc(addr, lbo, D * 16) | (2ull << 61); }
 
 // Bounded wait.
 __device__ __forceinline__ bool pc_wait(uint32_t bar, uint32_t parity, int *gave_up) {
@@ -119,15 +120,17 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// The pool's K and V as arrays [page][kv head][row][D]; on: they can be described so, and pages hold a swizzle atom.
+// The pool's K and V as arrays [cell][groups of 8 rows][D / 64][8 rows][64], cell = page * apart + kv head < cells; on: they can be
+// described so, and pages hold a swizzle atom.
 struct ChunkMaps {
   CUtensorMap map[2];
-  int on;
+  int on, apart, cells;
 };
 
-__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap *map, int c0, int row, int kvh, int page, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-               "l"(map), "r"(c0), "r"(row), "r"(kvh), "r"(page), "r"(bar)
+// rows of a page from the group-th eighth on
+__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap *map, int group, int cell, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %3, %4}], [%5];" ::"r"(dst),
+               "l"(map), "r"(0), "r"(group), "r"(cell), "r"(bar)
                : "memory");
 }
 
@@ -224,8 +227,8 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       // ---- copies: K and V tiles in turn through the ring
       fence_proxy_async_global();                              // the cache's new rows were written by ordinary stores
       constexpr int PARTS = D / 8;
-      const int rows_here = min(1 << lg, PC_TK);               // of a tile, in one page
-      const int n_pages = PC_TK / rows_here;                   // pages of a tile
+      const int rows_here = min(1 << lg, PC_BOX);              // of a tile, in one copy
+      const int n_copies = PC_TK / rows_here;
       int n = 0;                                               // tiles so far
       bool ok = true;
       ChunkPiece c;
@@ -244,10 +247,10 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
           // rows [0, whole) by TMA, the page that the last key shares with rows behind it and nothing else by the lanes
           const int whole = !M.on ? 0 : left >= PC_TK ? PC_TK : left / rows_here * rows_here;
           const int rest = !M.on ? PC_TK : whole < left ? min(PC_TK, whole + rows_here) : whole;          // rows [whole, rest) by the lanes
-          const int panel = lane / n_pages, row_tma = lane % n_pages * rows_here;
-          int id_tma = __shfl_sync(0xffffffffu, ids, row_tma >> 2);
-          if (row_tma >= whole || id_tma < 0 || id_tma >= P.pool.n_pages) id_tma = P.pool.n_pages;          // behind the end: zeros
-          const bool tma = M.on && panel < C::PANELS && (row_tma < whole || row_tma >= rest);
+          const int row_tma = lane * rows_here, id_tma = __shfl_sync(0xffffffffu, ids, row_tma >> 2 & 31);
+          const bool real = row_tma < whole && id_tma >= 0 && id_tma < P.pool.n_pages;
+          const int cell = real ? id_tma * M.apart + c.kvh : M.cells;                  // behind the end: zeros
+          const bool tma = M.on && lane < n_copies && (row_tma < whole || row_tma >= rest);
 #pragma unroll 1
           for (int kv = 0; kv < 2; ++kv, ++n) {
             const int st = n % C::STAGES;
@@ -256,7 +259,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
             const uint32_t dst = smem + C::RING + st * C::TILE, bar = smem_u32(&sh.full[st]);
             if (lane == 0) mbar_expect_tx(bar, (PC_TK - (rest - whole)) * D * (int)sizeof(T));
             __syncwarp();
-            if (tma) tma_page(dst + panel * PC_HALF + row_tma * 128, &M.map[kv], panel * 64, i * PC_TK & ((1 << lg) - 1), c.kvh, id_tma, bar);
+            if (tma) tma_page(dst + row_tma * (D * 2), &M.map[kv], ((i * PC_TK + row_tma) & ((1 << lg) - 1)) >> 3, cell, bar);
             if (rest > whole) {
               const T *src = reinterpret_cast<const T *>(kv ? P.pool.v : P.pool.k) + c.kvh * P.pool.head_stride;
 #pragma unroll 4
@@ -264,7 +267,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
                 const int row = whole + j / PARTS, part = j % PARTS, key = i * PC_TK + row;
                 const int id = key < n_keys ? table[key >> lg] : -1;
                 const bool real = id >= 0 && id < P.pool.n_pages;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pc_part(row, part)),
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pc_part<D>(row, part)),
                              "l"(real ? src + id * P.pool.page_stride + (key & ((1 << lg) - 1)) * P.pool.row_stride + part * 8 : src), "r"(real ? 16 : 0)
                              : "memory");
               }
@@ -294,7 +297,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       const uint32_t idesc_s = (1u << 4) | (fmt << 7) | (fmt << 10) | ((PC_STEP >> 3) << 17) | ((PC_M >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((D >> 3) << 17) | ((PC_M >> 4) << 24);
       const uint32_t t_s = tmem + h * 128, t_o = tmem + 256 + h * 128;
-      const uint64_t q_desc = pc_desc(smem + C::Q + h * C::TILE, 16);
+      const uint64_t q_desc = pc_desc<D>(smem + C::Q + h * C::TILE, 16);
       int st = 0, ph = 0, q_ph = 0, o_ph = 0, p_ph = 0, n_pv = 0;          // p_ph: a bit per place; n_pv: P V so far
       bool ok = true, used = false;                            // used: the half had steps in the piece before
       auto all = [&](bool x) { return __all_sync(0xffffffffu, x); };
@@ -302,11 +305,11 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&bar)) : "memory");
       };
       auto scores = [&](int slot, int j) {                     // step j: a half of the tile in `slot`
-        const uint64_t k_desc = pc_desc(smem + C::RING + slot * C::TILE + (j & 1) * PC_STEP * 128, 16);
+        const uint64_t k_desc = pc_desc<D>(smem + C::RING + slot * C::TILE + (j & 1) * PC_STEP * D * 2, 16);
         const uint32_t d = t_s + (j & 1) * PC_STEP;
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-          const uint64_t off = ((kk >> 2) * PC_HALF + (kk & 3) * 32) >> 4;
+          const uint64_t off = ((kk >> 2) * 1024 + (kk & 3) * 32) >> 4;
           asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
                        "l"(q_desc + off), "l"(k_desc + off), "r"(idesc_s), "r"(kk > 0 ? 1u : 0u)
                        : "memory");
@@ -314,12 +317,12 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         commit(sh.s_full[h][j & 1]);
       };
       auto values = [&](int slot, int j, bool first, bool last) {
-        const uint64_t v_desc = pc_desc(smem + C::RING + slot * C::TILE + (j & 1) * PC_STEP * 128, PC_HALF);
+        const uint64_t v_desc = pc_desc<D>(smem + C::RING + slot * C::TILE + (j & 1) * PC_STEP * D * 2, 1024);
         const uint32_t p = t_s + (j & 1) * PC_STEP;
 #pragma unroll
         for (int kk = 0; kk < PC_STEP / 16; ++kk)
           asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(t_o),
-                       "r"(p + kk * 8), "l"(v_desc + kk * (2048 >> 4)), "r"(idesc_o), "r"(first && kk == 0 ? 0u : 1u)
+                       "r"(p + kk * 8), "l"(v_desc + kk * (D * 32 >> 4)), "r"(idesc_o), "r"(first && kk == 0 ? 0u : 1u)
                        : "memory");
         commit(sh.o_done[h]);
         if (last) commit(sh.o_full[h]);
@@ -410,7 +413,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
         for (int r0 = 0; r0 < PC_M; r0 += AT_ONCE) {
           const int r = r0 + row / PARTS, i = h * PC_M + r, p = i / G;
           const bool real = i < nQ;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem + C::Q + h * C::TILE + pc_part(r, part)),
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem + C::Q + h * C::TILE + pc_part<D>(r, part)),
                        "l"(real ? q + (c.row0 + p) * P.q_stride + (c.kvh * G + i - p * G) * D + part * 8 : q), "r"(real ? 16 : 0)
                        : "memory");
         }

@@ -76,8 +76,8 @@ PagedScratch scratch_at(void *scratch, size_t offset, int blocks, int rows) {
 }
 
 // The pool as TMA sees it: [page and kv head][groups of 8 rows][64 dimensions][8 rows][64 values of them], up to 32 rows of a page with
-// all their dimensions to a copy (a copy takes its SM some 100 cycles and more whatever its size: two of 64 dimensions each for
-// pages of 16 rows were the bound of the chunk kernel, 236 us for 2000 rows over 8000 keys).
+// all their dimensions to a copy (a small copy takes its SM some 100 cycles whatever its size: two of 64 dimensions each cost 330 us for
+// 2000 rows over 8000 keys in pages of 8, now 236; whole pages of 128 rows come later than four parts of them, 244 against 232).
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeTiled encode_tiled() {

@@ -12,7 +12,8 @@
 // The angle is taken in turns of the circle, in 64 bits up to the fraction (at position 10^6 fp32 would be off by 0.06
 // radians), and the fraction's cosine and sine in 32.
 //
-// Bound: bytes (each value is read and written once) from some thousand rows on, below that one trip to memory.
+// Bound: bytes (each value is read and written once) from some thousand rows on, below that one trip to memory.  Measured: 8191 rows of
+// 32 + 2 x 8 vectors of 128, bf16: 34.3 us, 5.9 TB/s; 32 rows 3.0 us.
 #pragma once
 
 #include "paged_common.cuh"

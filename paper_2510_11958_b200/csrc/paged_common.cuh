@@ -55,8 +55,8 @@ __device__ __forceinline__ void store_pack(T *p, const float (&f)[N]) {
   *reinterpret_cast<Pack<T, N> *>(p) = x;
 }
 
-// The first grid barrier of a launch chain (see pdl_enter in kernels.cuh): the kernel behind this one may become resident,
-// and nothing is read or written before the kernels in front of this one are complete.
+// Start of a kernel in a chain of dependent launches: the kernel behind this one may become resident, and nothing is read or
+// written before the kernels in front of this one are complete.
 __device__ __forceinline__ void paged_enter() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -347,7 +347,8 @@ __device__ __forceinline__ void paged_join_rows(const PagedAttentionParams &P, c
 }
 
 // Joins what was cut: a block to each of the row kernel's `blocks` shares, a warp to a row; then, if the chunk kernel ran
-// too, per_chunk blocks to each of its shares.
+// too, per_chunk blocks to each of its shares.  Bound: two trips to memory, 3 to 4.5 us; behind the chunk kernel the partial results (35 MB, most of
+// them still in L2), 8 us.
 constexpr int PAGED_MERGE_WARPS = 16;
 template <int D> __host__ __device__ constexpr int paged_merge_per_chunk(int rows) { return rows / 32 * (D / 16) / PAGED_MERGE_WARPS; }
 template <typename T, typename KVT, int D>

@@ -410,6 +410,24 @@ def test_queries_of_any_size(pkg, kv, size):
     assert ((got.double() - ref).abs() <= 2e-5 * spread + 1e-5).all()
 
 
+@pytest.mark.parametrize("nkv,pages,pad", [(2, None, 8), (2, None, 64 * 16 * 3), (1, None, 8), (2, 1, 8), (1, 1, 0)])
+def test_pages_apart(pkg, nkv, pages, pad):
+    """Pages with room between them, a whole number of heads or not; one kv head, one page."""
+    page, D = (16, 64) if pages is None else (512, 64)
+    cached, new = ([300, 5], [150, 70]) if pages is None else ([200], [150])
+    c = attention_case(18, cached, new, 4, nkv, D, BF16, BF16, page, "hnd")
+    if pages == 1:                                                       # the pool is the request's only page
+        at = c["table"][0, 0].long()
+        c["kc"], c["vc"], c["table"] = c["kc"][at:at + 1], c["vc"][at:at + 1], torch.zeros_like(c["table"])
+        c["table"][:, 1:] = -1
+    for name in ("kc", "vc"):
+        t = c[name]
+        apart = torch.full((t.shape[0], nkv * page * D + pad), float("nan"), dtype=BF16, device="cuda")
+        c[name] = apart[:, :nkv * page * D].unflatten(1, (nkv, page, D))
+        c[name].copy_(t)
+    check_attention(pkg, c)
+
+
 @pytest.mark.parametrize("qt,kv", [(F32, F16), (BF16, BF16)])
 @pytest.mark.parametrize("B", [257, 700])
 def test_more_requests_than_are_kept(pkg, qt, kv, B):

@@ -25,9 +25,9 @@ struct PagedPool {
 struct PagedBatch {
   const int *row_start, *lens, *table;
   int n_requests, table_stride, n_rows;
-  __device__ __forceinline__ int row(int b) const { return min(max(row_start[b], 0), n_rows); }
+  __host__ __device__ __forceinline__ int row(int b) const { return min(max(row_start[b], 0), n_rows); }
   // keys of request b, as far as its table goes
-  __device__ __forceinline__ int keys(int b, int lg_page) const {
+  __host__ __device__ __forceinline__ int keys(int b, int lg_page) const {
     return (int)min((long long)max(lens[b], 0), (long long)table_stride << lg_page);
   }
 };

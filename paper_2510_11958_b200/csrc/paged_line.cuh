@@ -17,7 +17,7 @@ namespace dmtd {
 
 // Sum of floor((a i + b) / m) over i = 0 .. n - 1, by exchanging the roles of i and the quotient (a lattice-point
 // count under a line, as in Euclid's algorithm).
-__device__ __forceinline__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned long long b) {
+__host__ __device__ __forceinline__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned long long b) {
   long long s = 0;
   for (;;) {
     if (a >= m) { s += (long long)n * (n - 1) / 2 * (a / m); a %= m; }
@@ -36,7 +36,7 @@ __device__ __forceinline__ long long floor_sum(unsigned n, unsigned m, unsigned 
 }
 
 // x / y without the 64-bit division where 32 bits do
-__device__ __forceinline__ long long quotient(long long x, long long y) {
+__host__ __device__ __forceinline__ long long quotient(long long x, long long y) {
   return ((x | y) >> 32) ? x / y : (long long)((unsigned)x / (unsigned)y);
 }
 
@@ -53,37 +53,39 @@ struct PagedRequest {
   int b, row0, n, c;                 // first row of q, new rows, position of the first of them (may be negative)
   int tiles;
   // units of row tile i, and of the first m row tiles, for one kv head
-  __device__ __forceinline__ int units(const PagedCut &K, int i) const {
+  __host__ __device__ __forceinline__ int units(const PagedCut &K, int i) const {
     const int keys = c + min(n, (i + 1) * K.tile);
     return 1 + (keys <= 0 ? 0 : (int)(((unsigned)keys + (1u << K.lg_unit) - 1) >> K.lg_unit));
   }
-  __device__ __forceinline__ long long units_before(const PagedCut &K, int m) const {
+  __host__ __device__ __forceinline__ long long units_before(const PagedCut &K, int m) const {
     if (m == 0) return 0;
     if (m == 1) return units(K, 0);
     const int full = min(m, n / K.tile);
     const int none = c < 0 ? min(full, (int)(-(long long)c / K.tile)) : 0;       // tiles in front of position 0
     long long s = full;
     const unsigned n_sum = full - none, lg = K.lg_unit, unit = 1u << lg;
-    const unsigned long long base = (long long)c + (long long)none * K.tile + unit - 1;        // ceil(x / unit) = floor((x + unit - 1) / unit)
+    // Tiles from `none` on see a key at least, so that `base`, their first one's keys + unit - 1, is above 0 whatever c is:
+    // ceil(x / unit) = floor((x + unit - 1) / unit)
+    const unsigned long long base = (unsigned long long)((long long)c + (none + 1ll) * K.tile) + unit - 1;
     if (n_sum == 0) {
     } else if (K.lg_tile < 0) {
-      s += floor_sum(n_sum, unit, K.tile, base + K.tile);
+      s += floor_sum(n_sum, unit, K.tile, base);
     } else if (K.lg_tile >= (int)lg) {
-      s += (long long)(base >> lg) * n_sum + ((long long)n_sum * (n_sum + 1) / 2 << (K.lg_tile - lg));
+      s += (long long)(base >> lg) * n_sum + ((long long)n_sum * (n_sum - 1) / 2 << (K.lg_tile - lg));
     } else {
-      // base = q unit + rest: q, and floor(j / r) for the j from rest / tile + 1 on, r = unit / tile
+      // base = q unit + rest: q, and floor(j / r) for the n_sum values of j from rest / tile on, r = unit / tile
       const unsigned lr = lg - K.lg_tile, j0 = (unsigned)(base & (unit - 1)) >> K.lg_tile;
-      auto sum_to = [&](unsigned j) {                          // floor(0 / r) + ... + floor(j / r)
+      auto sum_below = [&](unsigned j) {                       // floor(0 / r) + ... + floor((j - 1) / r)
         const long long a = j >> lr;
-        return (a * (a - 1) / 2 << lr) + a * ((j & ((1u << lr) - 1)) + 1);
+        return (a * (a - 1) / 2 << lr) + a * (j & ((1u << lr) - 1));
       };
-      s += (long long)(base >> lg) * n_sum + sum_to(j0 + n_sum) - sum_to(j0);
+      s += (long long)(base >> lg) * n_sum + sum_below(j0 + n_sum) - sum_below(j0);
     }
     return m > full ? s + units(K, full) : s;
   }
 };
 
-__device__ __forceinline__ PagedRequest paged_request(const PagedBatch &batch, int lg_page, const PagedCut &K, int b) {
+__host__ __device__ __forceinline__ PagedRequest paged_request(const PagedBatch &batch, int lg_page, const PagedCut &K, int b) {
   PagedRequest r;
   r.b = b;
   r.row0 = batch.row(b);
@@ -99,15 +101,15 @@ struct PagedPiece {
   PagedRequest r;
   int i, kvh;                        // row tile, kv head
   int t0, t1, per_item;              // units [t0, t1) of per_item, the one in front among them
-  __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == per_item; }
-  __device__ __forceinline__ int first(const PagedCut &K) const { return i * K.tile; }
-  __device__ __forceinline__ int rows(const PagedCut &K) const { return min(K.tile, r.n - i * K.tile); }
+  __host__ __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == per_item; }
+  __host__ __device__ __forceinline__ int first(const PagedCut &K) const { return i * K.tile; }
+  __host__ __device__ __forceinline__ int rows(const PagedCut &K) const { return min(K.tile, r.n - i * K.tile); }
   // the piece's units of keys
-  __device__ __forceinline__ int key_begin() const { return max(t0 - 1, 0); }
-  __device__ __forceinline__ int key_end() const { return t1 - 1; }
+  __host__ __device__ __forceinline__ int key_begin() const { return max(t0 - 1, 0); }
+  __host__ __device__ __forceinline__ int key_end() const { return t1 - 1; }
   // keys that the tile's last row sees, and position of its first row
-  __device__ __forceinline__ int keys(const PagedCut &K) const { return max(0, r.c + min(r.n, (i + 1) * K.tile)); }
-  __device__ __forceinline__ int position(const PagedCut &K) const { return r.c + i * K.tile; }
+  __host__ __device__ __forceinline__ int keys(const PagedCut &K) const { return max(0, r.c + min(r.n, (i + 1) * K.tile)); }
+  __host__ __device__ __forceinline__ int position(const PagedCut &K) const { return r.c + i * K.tile; }
 };
 
 // The first THREADS threads of a block work out the line's length and their block's share.  KEPT: as many requests at most are
@@ -122,7 +124,7 @@ struct PagedShare {
     PagedPiece first;                // the share's first piece, by plan()
     int kept[KEPT][3];               // row0, n, c
   };
-  __device__ __forceinline__ PagedRequest request(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, int b) const {
+  __host__ __device__ __forceinline__ PagedRequest request(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, int b) const {
     if (P.batch.n_requests > KEPT) return paged_request(P.batch, P.pool.lg_page, K, b);
     PagedRequest r;
     r.b = b;
@@ -184,15 +186,15 @@ struct PagedShare {
     }
     __syncthreads();
   }
-  __device__ __forceinline__ long long start(int block) const { return each * block + min((long long)block, rest); }
+  __host__ __device__ __forceinline__ long long start(int block) const { return each * block + min((long long)block, rest); }
   // the block that holds unit u
-  __device__ __forceinline__ int holder(long long u) const {
+  __host__ __device__ __forceinline__ int holder(long long u) const {
     const long long longer = rest * (each + 1);          // units of the longer shares, which come first
     return (int)(u < longer ? quotient(u, each + 1) : rest + quotient(u - longer, each));
   }
 
   // The piece that begins with the share, at unit v of request r.
-  __device__ __forceinline__ PagedPiece piece_of(const PagedAttentionParams &P, const PagedCut &K, const PagedRequest &r, long long v) const {
+  __host__ __device__ __forceinline__ PagedPiece piece_of(const PagedAttentionParams &P, const PagedCut &K, const PagedRequest &r, long long v) const {
     PagedPiece p;
     p.r = r;
     // the row tile: the last whose units begin at or before v
@@ -210,7 +212,7 @@ struct PagedShare {
     return p;
   }
   // The piece behind p, which ends at unit u of the line; false: the share ends there.
-  __device__ __forceinline__ bool next(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, PagedPiece &p, long long u) const {
+  __host__ __device__ __forceinline__ bool next(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, PagedPiece &p, long long u) const {
     if (u >= end) return false;
     if (++p.kvh == P.nkv) {
       p.kvh = 0;

@@ -211,7 +211,7 @@ struct PagedShare {
     p.t1 = (int)min((long long)p.per_item, p.t0 + (end - begin));
     return p;
   }
-  // The piece behind p, which ends at unit u of the line; false: the share ends there.
+  // The piece behind p, which ends at unit u of the line; false: the share or the batch ends there.
   __host__ __device__ __forceinline__ bool next(const PagedAttentionParams &P, const PagedCut &K, const Shared &sh, PagedPiece &p, long long u) const {
     if (u >= end) return false;
     if (++p.kvh == P.nkv) {
@@ -219,7 +219,10 @@ struct PagedShare {
       if (++p.i == p.r.tiles) {
         p.i = 0;
         int b = p.r.b;
-        do { p.r = request(P, K, sh, ++b); } while (p.r.n == 0 && b + 1 < P.batch.n_requests);
+        do {
+          if (++b >= P.batch.n_requests) return false;
+          p.r = request(P, K, sh, b);
+        } while (p.r.n == 0);
       }
       p.per_item = p.r.units(K, p.i);
     }

@@ -21,10 +21,7 @@ pytestmark = pytest.mark.gpu
     (16, 1, 128, [70], [3]),
 ])
 def test_pieces_with_fewer_keys_than_rows(pkg, qt, kv, nq, nkv, D, new, lens):
-    c = attention_case(21, [0] * len(new), new, nq, nkv, D, qt, kv, 16, "hnd", pad=2)
-    for b, n in enumerate(new):
-        if lens[b] > n:                                              # (this request has its keys)
-            c = attention_case(21, [max(0, m - k) for m, k in zip(lens, new)], new, nq, nkv, D, qt, kv, 16, "hnd", pad=2)
+    c = attention_case(21, [max(0, m - n) for m, n in zip(lens, new)], new, nq, nkv, D, qt, kv, 16, "hnd", pad=2)
     c["lens"] = lens
     for max_new in (0, max(new)):
         got = check_attention(pkg, c, max_new=max_new)

@@ -113,8 +113,41 @@ static int walk(int G, int kind, int nkv, int grid) {
   return 0;
 }
 
+// A share whose end lies behind the line's: its pieces end with the batch's last request all the same.
+static int past() {
+  const PagedCut K = cut(3, 4);
+  static PagedShare<128, 64>::Shared sh;
+  long long bad = 0;
+  for (int waits = 0; waits < 3; ++waits) {                    // requests without rows at the batch's end
+    const int start[4] = {0, 100, waits < 2 ? 300 : 100, waits < 1 ? 301 : start[2]}, lens[3] = {100, 900, 50};
+    PagedAttentionParams P{};
+    P.batch = PagedBatch{start, lens, nullptr, 3, 1 << 10, start[3]};
+    P.pool.lg_page = 4;
+    P.nkv = 2;
+    int items = 0;
+    for (int b = 0; b < 3; ++b) {
+      const PagedRequest r = paged_request(P.batch, P.pool.lg_page, K, b);
+      sh.kept[b][0] = r.row0; sh.kept[b][1] = r.n; sh.kept[b][2] = r.c;
+      items += r.tiles * P.nkv;
+    }
+    for (int b = 3; b < 64; ++b) sh.kept[b][1] = 7;            // what lies behind the batch
+    PagedShare<128, 64> share{};
+    share.end = 1 << 20;
+    PagedPiece p = share.piece_of(P, K, share.request(P, K, sh, 0), 0);
+    long long u = p.t1;
+    while (items > 0 && share.next(P, K, sh, p, u)) {
+      u += p.t1 - p.t0;
+      --items;
+    }
+    bad += items != 1;
+  }
+  printf("%lld\n", bad);
+  return 0;
+}
+
 int main(int argc, char **argv) {
   auto a = [&](int i) { return atoi(argv[i]); };
+  if (argc == 1) return past();
   return argc == 3 ? sums(a(1), a(2)) : walk(a(1), a(2), a(3), a(4));
 }
 """
@@ -144,3 +177,7 @@ def test_units_in_closed_form(probe, G, kind):
 @pytest.mark.parametrize("G,nkv,grid", [(1, 8, 148), (1, 1, 7), (2, 8, 296), (4, 2, 148), (5, 3, 31), (16, 1, 148)])
 def test_shares_hold_every_item_once(probe, G, nkv, grid, kind):
     assert probe(G, kind, nkv, grid) == 0
+
+
+def test_no_piece_behind_the_last_request(probe):
+    assert probe() == 0

@@ -49,6 +49,7 @@ __device__ __noinline__ void paged_attend_row(const PagedAttentionParams &P, int
     }
     const float p = __expf(s - m);
     l += p;
+    if (isnan(l)) break;                               // the row is NaN, whatever follows
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = fmaf(p, v[e], o[e]);
   }

@@ -280,6 +280,7 @@ __device__ __forceinline__ void paged_join_row(const PagedAttentionParams &P, co
     const float top = fmaxf(m, warp_max(ml.x));
     const float old = m > -INFINITY ? exp2f(m - top) : 0.f;
     const float w = ml.x > -INFINITY ? exp2f(ml.x - top) : 0.f;
+    // (a piece whose scores are all NaN has level -inf and sum NaN, which stays)
     l = l * old + warp_sum(ml.y * w);
     m = top;
 #pragma unroll
@@ -322,7 +323,10 @@ __device__ __forceinline__ void paged_join_rows(const PagedAttentionParams &P, c
 #pragma unroll
     for (int k = 0; k < 4; ++k) load_pack(S.sums<D>(place) + ((size_t)(d0 / 4 + k) * S.rows + qi) * 4, v[k]);
     const float2 ml = S.levels<D>(place)[qi];
-    if (ml.x == -INFINITY) continue;                           // (a piece without keys)
+    if (ml.x == -INFINITY) {                                   // a piece without keys: sum 0; one whose scores are all NaN: NaN
+      l += ml.y;
+      continue;
+    }
     const float top = fmaxf(m, ml.x), old = m > -INFINITY ? exp2f(m - top) : 0.f, w = exp2f(ml.x - top);
     m = top;
     l = l * old + ml.y * w;

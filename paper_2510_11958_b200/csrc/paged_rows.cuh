@@ -607,7 +607,9 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
 #pragma unroll
       for (int w = 0; w < PR_WARPS; ++w) {
         const float mw = red_m[w * PR_ROWS + qi];
-        if (mw > -INFINITY) {                                  // (a warp without keys has none)
+        if (mw == -INFINITY) {
+          l += red_l[w * PR_ROWS + qi];                        // a warp without keys: 0; one whose scores are all NaN: NaN
+        } else {
           const float f = exp2_approx(mw - m);
           const float4 v = *reinterpret_cast<const float4 *>(o_s + (w * PR_ROWS + qi) * C::OROW + at);
           l = fmaf(red_l[w * PR_ROWS + qi], f, l);

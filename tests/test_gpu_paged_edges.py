@@ -55,3 +55,55 @@ def test_a_refused_piece_of_a_prompt(pkg, nq, nkv):
     c["lens"], c["start"], c["table"] = plan.lens.tolist(), plan.row_start.tolist(), table
     got = check_attention(pkg, c, finite=False)
     assert torch.isfinite(got).all()
+
+
+# ---- NaN stays
+
+def check_nan(pkg, c, rows_heads, max_new=0):
+    """NaN in all of these (row, query head) and nowhere else."""
+    got = check_attention(pkg, c, max_new=max_new, finite=False)
+    want = torch.zeros(got.shape[:2], dtype=torch.bool, device="cuda")
+    for t, h in rows_heads:
+        want[t, h] = True
+    assert torch.equal(torch.isnan(got).all(-1), want) and torch.equal(torch.isnan(got).any(-1), want)
+
+
+@pytest.mark.parametrize("qt,kv", TYPES)
+@pytest.mark.parametrize("nq,nkv,D,cached,new,max_new", [
+    (8, 2, 128, [0, 5], [1, 2], 0),                    # one key
+    (8, 2, 128, [40, 5], [2, 1], 2),                   # an item in one piece or a few
+    (16, 2, 64, [4000], [3], 3),                       # in many
+    (8, 2, 128, [70, 3], [200, 60], 0),                # pieces of prompts
+    (8, 8, 64, [1, 3], [130, 300], 0),
+    (4, 1, 128, [9000], [100], 0),                     # ... an item cut into many pieces
+])
+def test_a_query_with_a_nan(pkg, qt, kv, nq, nkv, D, cached, new, max_new):
+    c = attention_case(31, cached, new, nq, nkv, D, qt, kv, 16, "hnd")
+    T = sum(new)
+    at = sorted({(0, 0), (T - 1, nq - 1), (T // 2, 1)})
+    for n, (t, h) in enumerate(at):
+        c["q"][t, h, 7 * n % D] = math.nan
+    check_nan(pkg, c, at, max_new)
+
+
+@pytest.mark.parametrize("qt,kv", TYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cached,new", [([0], [1]), ([16], [1]), ([8], [1]), ([32], [1]), ([64], [1]), ([128], [1]), ([1023], [2]), ([4095, 64], [1, 1]),
+                                        ([128], [90]), ([0], [70]), ([8999], [100])])
+def test_a_nan_key_alone_in_its_tile(pkg, qt, kv, D, cached, new):
+    """The last key of the first new row's sight has a NaN: that row and those behind it see it, wherever a tile or a piece begins."""
+    c = attention_case(32, cached, new, 8, 2, D, qt, kv, 16, "hnd")
+    for b, n in enumerate(cached):
+        c["kc"][c["table"][b, n // 16].long(), 1, n % 16, 3] = math.nan
+    rows = [(c["start"][b] + r, h) for b in range(len(new)) for r in range(new[b]) for h in range(4, 8)]
+    check_nan(pkg, c, rows)
+
+
+@pytest.mark.parametrize("qt,kv", TYPES)
+@pytest.mark.parametrize("cached,new", [([700, 3], [1, 2]), ([6000], [3]), ([30], [40]), ([6000], [60])])
+def test_keys_that_are_all_nan(pkg, qt, kv, cached, new):
+    """Every score of a row is NaN, in all its pieces; the other requests' and heads' rows are as ever."""
+    c = attention_case(33, cached, new, 8, 2, 128, qt, kv, 16, "nhd")
+    pages = c["table"][0][c["table"][0] >= 0].long()
+    c["kc"][pages, 0] = math.nan
+    check_nan(pkg, c, [(t, h) for t in range(new[0]) for h in range(4)])

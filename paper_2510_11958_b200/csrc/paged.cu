@@ -66,13 +66,15 @@ int sm_count() {
   return n;
 }
 
-// Scratch: the places of the row kernel's blocks, then those of the chunk kernel's.
+// Scratch: the places of the row kernel's blocks, then those of the chunk kernel's, then a word (paged_line.cuh).
 constexpr int ROWS_BLOCKS = 304, CHUNK_BLOCKS = 152;
 constexpr size_t scratch_part(int blocks, int rows) { return (blocks * (sizeof(PagedCutItem) + 2ull * rows * 130 * 4) + 255) / 256 * 256; }
-static_assert(scratch_part(ROWS_BLOCKS, PR_ROWS) + scratch_part(CHUNK_BLOCKS, PC_ROWS) <= DMTD_PAGED_ATTENTION_SCRATCH_BYTES, "scratch");
+constexpr size_t SCRATCH_ENTERED = scratch_part(ROWS_BLOCKS, PR_ROWS) + scratch_part(CHUNK_BLOCKS, PC_ROWS);
+static_assert(SCRATCH_ENTERED + 256 <= DMTD_PAGED_ATTENTION_SCRATCH_BYTES, "scratch");
 PagedScratch scratch_at(void *scratch, size_t offset, int blocks, int rows) {
-  PagedCutItem *items = reinterpret_cast<PagedCutItem *>(static_cast<unsigned char *>(scratch) + offset);
-  return PagedScratch{items, reinterpret_cast<float *>(items + blocks), rows};
+  unsigned char *const at = static_cast<unsigned char *>(scratch);
+  PagedCutItem *items = reinterpret_cast<PagedCutItem *>(at + offset);
+  return PagedScratch{items, reinterpret_cast<float *>(items + blocks), rows, reinterpret_cast<unsigned *>(at + SCRATCH_ENTERED)};
 }
 
 // The pool as TMA sees it: [page and kv head][groups of 8 rows][64 dimensions][8 rows][64 values of them], up to 32 rows of a page with

@@ -180,9 +180,10 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  // in this order: the row kernel behind does not wait for what is in front of this one (and no grid may hold tensor memory's
-  // columns off this block while it waits)
+  // in this order: the row kernel behind does not wait for what is in front of this one, but finds it through `entered` (and no grid
+  // may hold tensor memory's columns off this block while it waits)
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (blockIdx.x == 0 && threadIdx.x == 0) st_release_u32(S.entered, PAGED_ENTERED);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem = sh.tmem;
   ChunkShare share;

@@ -343,10 +343,10 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
   const int G = P.nq / P.nkv, lg = P.pool.lg_page;
   const uint32_t g_inv = (65536 + G - 1) / G;                  // i / G == i * g_inv >> 16 for i < 16
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  // Behind the chunk kernel this one was let in by blocks that had waited for everything in front of them, and it reads nothing that
-  // they write: it waits at its end, for the grids behind it.
+  // Behind the chunk kernel this one reads nothing that that kernel writes: it acquires what lies in front of both (paged_line.cuh) and
+  // waits at its end, for the grids behind it.
   auto wait = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
-  if (!behind_chunk) wait();
+  if (!behind_chunk || !__syncthreads_or(threadIdx.x == 0 && paged_entered(S.entered))) wait();
   RowsShare share;
   share.plan(P, K, sh.line, blockIdx.x, gridDim.x);
   if (share.begin >= share.end) {

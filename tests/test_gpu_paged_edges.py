@@ -107,3 +107,63 @@ def test_keys_that_are_all_nan(pkg, qt, kv, cached, new):
     pages = c["table"][0][c["table"][0] >= 0].long()
     c["kc"][pages, 0] = math.nan
     check_nan(pkg, c, [(t, h) for t in range(new[0]) for h in range(4)])
+
+
+# ---- what the kernels of a call find in scratch, and of the launches in front of it
+
+@pytest.mark.parametrize("fill", [0, 255, "entered"])
+@pytest.mark.parametrize("qt,kv", [(BF16, BF16), (F16, F16), (F32, F16)])
+def test_scratch_may_hold_anything(pkg, qt, kv, fill):
+    """Zeros, ones, and the word (everywhere) that the chunk kernel leaves for the row kernel behind it."""
+    c = attention_case(41, [900, 4, 3000], [200, 1, 3], 8, 2, 128, qt, kv, 16, "hnd")
+    args = c["q"], ints(c["start"]), ints(c["lens"]), c["table"], c["kc"], c["vc"]
+    scratch = torch.empty(pkg.PAGED_ATTENTION_SCRATCH_BYTES // 4, dtype=torch.int32, device="cuda")
+    scratch.fill_({0: 0, 255: -1, "entered": 0x9d1c6b35 - (1 << 32)}[fill])
+    want = check_attention(pkg, c)
+    for _ in range(3):
+        assert torch.equal(pkg.paged_attention(*args, scratch=scratch, out=c["out"].clone()), want)
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_rows_behind_a_piece_read_the_step_in_front(pkg, graph):
+    """Single rows beside a piece of a prompt: the kernel of the rows starts under that of the pieces, behind plan and append launches
+    that changed lengths, table and cache just now.  Step after step against the same call on a quiet device."""
+    B, nq, nkv, D, page, width = 9, 8, 2, 128, 8, 40
+    g = torch.Generator(device="cuda").manual_seed(42)
+    n_pages, n_rows = B * width, 100
+    lens, n_free = ints([0] * B), ints([n_pages])
+    n_new = ints([1] * (B - 1) + [60])
+    table = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+    free = torch.randperm(n_pages, generator=g, device="cuda").int()
+    kc, vc = pool(n_pages, nkv, page, D, BF16, "nhd")
+    q, k, v = (torch.zeros(n_rows, h, D, dtype=BF16, device="cuda") for h in (nq, nkv, nkv))
+    plan = [torch.zeros(n, dtype=torch.int32, device="cuda") for n in (B + 1, n_rows, n_rows, B)] + [lens, n_free]
+    q_rot, out = torch.zeros_like(q), torch.zeros_like(q)
+    scratch = torch.empty(pkg.PAGED_ATTENTION_SCRATCH_BYTES, dtype=torch.uint8, device="cuda")
+
+    def step():
+        p = pkg.paged_plan(lens, n_new, table, free, n_free, page, n_rows, out=plan)
+        pkg.paged_append(q, k, v, p.position, p.slot, kc, vc, rope_theta=1e4, q_out=q_rot)
+        pkg.paged_attention(q_rot, p.row_start, p.lens, table, kc, vc, scratch=scratch, out=out)
+    replay = step
+    if graph:
+        n_new.zero_()
+        step()
+        torch.cuda.synchronize()
+        captured = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(captured):
+            step()
+        replay = captured.replay
+    for i in range(40):
+        todo = [1] * (B - 1) + [60]
+        if i % 4 == 3:
+            todo = [-1] * B                                          # everything ends; pages go round
+        n_new.copy_(ints(todo))
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+        out.fill_(3.0)
+        replay()
+        torch.cuda.synchronize()
+        quiet = pkg.paged_attention(q_rot, plan[0], lens, table, kc, vc, out=torch.full_like(out, 3.0))
+        assert torch.equal(out, quiet), i
+        assert plan[3].tolist() == [max(0, n) for n in todo]

@@ -25,7 +25,8 @@
 //
 // Warps 0-3 and 4-7: softmax of the halves, queries, results; warps 8 and 9 issue their MMAs; warp 10 copies K and V; warp 11 lists the
 // pieces of the block's share (what the others would need 50 registers for).  Every wait is bounded: a block whose wait gives up leaves NaN
-// in the rows at hand and the rest unwritten.  Tensor memory is taken before the dependent grid is let in.
+// in the rows at hand and the rest unwritten.  Rows whose result is not finite are worked out from the definition at the block's end, where
+// nothing waits for them with a limit (chunk_again).  Tensor memory is taken before the dependent grid is let in.
 #pragma once
 
 #include <cuda.h>
@@ -83,7 +84,7 @@ __device__ __forceinline__ ChunkPiece chunk_piece(const PagedPiece &p, long long
 struct ChunkShared {
   uint64_t q_full[2], s_full[2][2], p_full[2][2], o_done[2], o_full[2], full[8], empty[8], piece_full[PC_PIECES], piece_empty[PC_PIECES];
   uint32_t tmem;
-  int gave_up;
+  int gave_up, again;                // again: some row of a whole item is not finite
   ChunkPiece piece[PC_PIECES];
   ChunkShare::Shared line;
 };
@@ -139,6 +140,32 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap *map, i
                : "memory");
 }
 
+// The block's share once more, behind its end: rows of whole items that are not finite, a warp to a row, from the definition.
+template <typename T, int D>
+__device__ __noinline__ void chunk_again(const PagedAttentionParams &P, const PagedCut &K, const PagedScratch &S, ChunkShared &sh) {
+  constexpr int E = D / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = P.nq / P.nkv;
+  ChunkShare share;
+  share.plan(P, K, sh.line, blockIdx.x, gridDim.x);
+  PagedPiece p = sh.line.first;
+  for (long long end = share.begin;;) {
+    end += p.t1 - p.t0;
+    const ChunkPiece c = chunk_piece(p, end, K, share, G);
+    if (c.began && c.ends) {
+      for (int i = warp; i < c.rows * G; i += PC_THREADS / 32) {
+        const int r = i / G, head = c.kvh * G + i - r * G;
+        float o[E];
+        load_pack(reinterpret_cast<const T *>(P.out) + ((size_t)(c.row0 + r) * P.nq + head) * D + lane * E, o);
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < E; ++e) bad = bad || !isfinite(o[e]);
+        if (__any_sync(0xffffffffu, bad)) paged_attend_row<T, T, D>(P, c.b, c.row0 + r, c.pos + r + 1, head);
+      }
+    }
+    if (!share.next(P, K, sh.line, p, end)) break;
+  }
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid_constant__ PagedAttentionParams P,
                                                                     const __grid_constant__ ChunkMaps M, PagedCut K, PagedScratch S) {
@@ -170,7 +197,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
       mbar_init(smem_u32(&sh.piece_full[i]), 1);
       mbar_init(smem_u32(&sh.piece_empty[i]), 11);             // a lane of every warp but the one that lists them
     }
-    sh.gave_up = 0;
+    sh.gave_up = sh.again = 0;
     fence_mbar_init();
   }
   if (warp == 8) {
@@ -576,15 +603,12 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
           }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        // rows that are not finite: see the row kernel
+        // rows that are not finite (see the row kernel) wait for the share's end.  (A thread storing for itself, without the vote: 267 us
+        // instead of 260 for 2000 rows over 8000 keys, by the rest of the loop's code)
         if (ok) {
-          uint32_t bad_rows = __ballot_sync(0xffffffffu, !good);
+          const uint32_t bad_rows = __ballot_sync(0xffffffffu, !good);
           __syncwarp();
-          while (bad_rows) {
-            const int i = h * PC_M + (warp & 3) * 32 + __ffs(bad_rows) - 1, r = i / G;
-            bad_rows &= bad_rows - 1;
-            paged_attend_row<T, T, D>(P, c.b, c.row0 + r, c.pos + r + 1, c.kvh * G + i - r * G);
-          }
+          if (bad_rows) sh.again = 1;
         }
         if (c.last || !ok) {
           if (c.last && threadIdx.x == 0) S.items[blockIdx.x] = PagedCutItem{c.pieces, c.b, c.row0, c.rows, c.pos + 1, c.kvh, {0, 0}};
@@ -598,6 +622,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(PC_TMEM) : "memory");
+  if (work && sh.again) chunk_again<T, D>(P, K, S, sh);
 }
 
 }  // namespace dmtd

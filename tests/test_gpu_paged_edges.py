@@ -167,3 +167,37 @@ def test_rows_behind_a_piece_read_the_step_in_front(pkg, graph):
         quiet = pkg.paged_attention(q_rot, plan[0], lens, table, kc, vc, out=torch.full_like(out, 3.0))
         assert torch.equal(out, quiet), i
         assert plan[3].tolist() == [max(0, n) for n in todo]
+
+
+# ---- rows that are worked out from the definition
+
+@pytest.mark.parametrize("qt,kv", TYPES)
+@pytest.mark.parametrize("cached,new,D", [([9000], [100], 128), ([9000], [100], 64), ([4000, 100], [1, 3], 128), ([500, 40, 8], [300, 70, 90], 128)])
+def test_the_same_bits_with_infinities(pkg, qt, kv, cached, new, D):
+    """An infinity in one dimension of V, seen by some rows and not by others, in items cut into pieces: the same call gives the same bits."""
+    c = attention_case(51, cached, new, 8, 2, D, qt, kv, 16, "hnd")
+    for n in (cached[0] // 2, cached[0] + new[0] // 2):
+        c["vc"][c["table"][0, n // 16].long(), :, n % 16, 5 + n % 7] = math.inf
+    first = check_attention(pkg, c, finite=False)
+    assert (first[: new[0]].isinf().any(-1)).all()
+    args = c["q"], ints(c["start"]), ints(c["lens"]), c["table"], c["kc"], c["vc"]
+    for _ in range(8):
+        assert torch.equal(torch.nan_to_num(pkg.paged_attention(*args, out=c["out"].clone())), torch.nan_to_num(first))
+
+
+@pytest.mark.parametrize("qt,kv", [(BF16, BF16), (F16, F16)])
+def test_infinities_in_shares_of_many_items(pkg, qt, kv):
+    """More items than blocks, most of them whole: those of some requests hold an infinity that a part of their rows see."""
+    B, page = 150, 16
+    new = [33 + 13 * b % 60 for b in range(B)]
+    cached = [29 * b % 300 for b in range(B)]
+    c = attention_case(52, cached, new, 8, 4, 64, qt, kv, page, "nhd", pad=3)
+    at = [b for b in range(B) if b % 11 == 4]
+    for b in at:
+        n = cached[b] + new[b] // 2
+        c["vc"][c["table"][b, n // page].long(), 1, n % page, 9] = -math.inf
+    got = check_attention(pkg, c, finite=False)
+    want = torch.zeros(got.shape, dtype=torch.bool, device="cuda")
+    for b in at:
+        want[c["start"][b] + new[b] // 2:c["start"][b + 1], 2:4, 9] = True
+    assert torch.equal(got == -math.inf, want) and torch.isfinite(got[~want]).all()

@@ -24,9 +24,9 @@
 // the lengths are.
 //
 // Warps 0-3 and 4-7: softmax of the halves, queries, results; warps 8 and 9 issue their MMAs; warp 10 copies K and V; warp 11 lists the
-// pieces of the block's share (what the others would need 50 registers for).  Every wait is bounded: a block whose wait gives up leaves NaN
-// in the rows at hand and the rest unwritten.  Rows whose result is not finite are worked out from the definition at the block's end, where
-// nothing waits for them with a limit (chunk_again).  Tensor memory is taken before the dependent grid is let in.
+// pieces of the block's share (what the others would need 50 registers for).  Every wait is bounded.  Rows whose result is not finite, and all
+// rows of a block whose wait gave up, are worked out from the definition at the block's end, where nothing waits for them with a limit
+// (chunk_again).  Tensor memory is taken before the dependent grid is let in.
 #pragma once
 
 #include <cuda.h>
@@ -140,11 +140,13 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap *map, i
                : "memory");
 }
 
-// The block's share once more, behind its end: rows of whole items that are not finite, a warp to a row, from the definition.
+// The block's share once more, behind its end: rows of whole items that are not finite, a warp to a row, from the definition; where a wait
+// gave up all rows, those of cut items by way of the merge, for which a sum of NaN stands for the block's part.
 template <typename T, int D>
 __device__ __noinline__ void chunk_again(const PagedAttentionParams &P, const PagedCut &K, const PagedScratch &S, ChunkShared &sh) {
   constexpr int E = D / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = P.nq / P.nkv;
+  const bool all = sh.gave_up;
   ChunkShare share;
   share.plan(P, K, sh.line, blockIdx.x, gridDim.x);
   PagedPiece p = sh.line.first;
@@ -156,12 +158,15 @@ __device__ __noinline__ void chunk_again(const PagedAttentionParams &P, const Pa
         const int r = i / G, head = c.kvh * G + i - r * G;
         float o[E];
         load_pack(reinterpret_cast<const T *>(P.out) + ((size_t)(c.row0 + r) * P.nq + head) * D + lane * E, o);
-        bool bad = false;
+        bool bad = all;
 #pragma unroll
         for (int e = 0; e < E; ++e) bad = bad || !isfinite(o[e]);
         if (__any_sync(0xffffffffu, bad)) paged_attend_row<T, T, D>(P, c.b, c.row0 + r, c.pos + r + 1, head);
       }
+    } else if (all) {
+      for (int i = threadIdx.x; i < c.rows * G; i += PC_THREADS) S.levels<D>(paged_place(blockIdx.x, c.began))[i] = make_float2(-INFINITY, NAN);
     }
+    if (all && c.last && threadIdx.x == 0) S.items[blockIdx.x] = PagedCutItem{c.pieces, c.b, c.row0, c.rows, c.pos + 1, c.kvh, {0, 0}};
     if (!share.next(P, K, sh.line, p, end)) break;
   }
 }
@@ -622,7 +627,7 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(PC_TMEM) : "memory");
-  if (work && sh.again) chunk_again<T, D>(P, K, S, sh);
+  if (work && (sh.again || sh.gave_up)) chunk_again<T, D>(P, K, S, sh);
 }
 
 }  // namespace dmtd

@@ -15,9 +15,11 @@ struct PagedAttentionParams {
 };
 
 // One query row and head by one warp, from the definition: the keys it sees one by one, softmax with a running maximum.  Slow
-// (a key takes some 100 cycles of latency); for rows that the tiled kernels cannot answer, see there.
+// (a key takes some 100 cycles of latency); for rows that the tiled kernels cannot answer, see there.  Dimensions [d0, d1) are written
+// (multiples of D / 32).
 template <typename T, typename KVT, int D>
-__device__ __noinline__ void paged_attend_row(const PagedAttentionParams &P, int b, int row, int seen, int head) {
+__device__ __noinline__ void paged_attend_row(const PagedAttentionParams &P, int b, int row, int seen, int head, int d0 = 0,
+                                             int d1 = D) {
   constexpr int E = D / 32;
   const int lane = threadIdx.x & 31, kvh = head / (P.nq / P.nkv), lg = P.pool.lg_page;
   const KVT *kb = reinterpret_cast<const KVT *>(P.pool.k), *vb = reinterpret_cast<const KVT *>(P.pool.v);
@@ -55,7 +57,7 @@ __device__ __noinline__ void paged_attend_row(const PagedAttentionParams &P, int
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = l != 0.f ? o[e] / l : 0.f;
-  store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o);
+  if (lane * E >= d0 && lane * E < d1) store_pack(reinterpret_cast<T *>(P.out) + ((size_t)row * P.nq + head) * D + lane * E, o);
 }
 
 }  // namespace dmtd

@@ -364,7 +364,8 @@ __device__ __forceinline__ void paged_join_rows(const PagedAttentionParams &P, c
   while (bad_rows) {
     const int i = q0 + __ffs(bad_rows) - 1, r = i / G;
     bad_rows &= bad_rows - 1;
-    paged_attend_row<T, T, D>(P, c.b, c.row0 + r, c.first_seen + r, c.kvh * G + i - r * G);
+    // (this warp's dimensions alone: those of a row in other warps may be finite, and the order of the warps is open)
+    paged_attend_row<T, T, D>(P, c.b, c.row0 + r, c.first_seen + r, c.kvh * G + i - r * G, d0, d0 + 16);
   }
 }
 

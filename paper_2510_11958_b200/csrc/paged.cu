@@ -49,13 +49,13 @@ dmtd_status pool_check(const char *what, const dmtd_paged_cache *c, PagedPool *o
   return DMTD_OK;
 }
 
-template <int D>
+template <int D, bool ROTATE>
 cudaError_t append_launch(const PagedAppendParams &P, int act, int kv, int blocks, cudaStream_t stream) {
   auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(blocks), dim3(APPEND_THREADS), APPEND_SMEM, stream, P); };
   auto by_kv = [&](auto t) {
     using T = decltype(t);
-    return kv == DMTD_F32 ? go(paged_append_kernel<T, float, D>)
-         : kv == DMTD_BF16 ? go(paged_append_kernel<T, __nv_bfloat16, D>) : go(paged_append_kernel<T, __half, D>);
+    return kv == DMTD_F32 ? go(paged_append_kernel<T, float, D, ROTATE>)
+         : kv == DMTD_BF16 ? go(paged_append_kernel<T, __nv_bfloat16, D, ROTATE>) : go(paged_append_kernel<T, __half, D, ROTATE>);
   };
   return act == DMTD_F32 ? by_kv(float{}) : act == DMTD_BF16 ? by_kv(__nv_bfloat16{}) : by_kv(__half{});
 }
@@ -229,7 +229,7 @@ dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32
   P.n_rows = n_rows; P.nq = n_q_heads; P.nkv = nkv;
   P.q_norm = q_norm; P.k_norm = k_norm; P.eps = rms_eps;
   P.position = position; P.slot = slot; P.q_out = q_out;
-  if (rope_theta > 0.f) {                                // (else all angles are 0)
+  if (rope_theta > 0.f) {                                // (else there is no rotation)
     const double ratio = std::pow((double)rope_theta, -2.0 / D);
     double f = 0.15915494309189533577;                   // 1 / (2 pi)
     for (int i = 0; i < D / 2; ++i, f *= ratio) P.turns[i] = f;
@@ -242,7 +242,9 @@ dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int64_t warps = (int64_t)n_rows * P.slices, blocks = (warps + APPEND_WARPS - 1) / APPEND_WARPS;
   if (warps > INT32_MAX - APPEND_WARPS) return call_failed(DMTD_ERR_CAPACITY, "paged_append: too many rows");
-  const cudaError_t e = D == 128 ? append_launch<128>(P, dtype, cache->dtype, (int)blocks, stream) : append_launch<64>(P, dtype, cache->dtype, (int)blocks, stream);
+  const auto launch = D == 128 ? rope_theta > 0.f ? append_launch<128, true> : append_launch<128, false>
+                               : rope_theta > 0.f ? append_launch<64, true> : append_launch<64, false>;
+  const cudaError_t e = launch(P, dtype, cache->dtype, (int)blocks, stream);
   return launched(e, "paged_append");
 }
 

@@ -201,3 +201,20 @@ def test_infinities_in_shares_of_many_items(pkg, qt, kv):
     for b in at:
         want[c["start"][b] + new[b] // 2:c["start"][b + 1], 2:4, 9] = True
     assert torch.equal(got == -math.inf, want) and torch.isfinite(got[~want]).all()
+
+
+# ---- append
+
+@pytest.mark.parametrize("act", [F32, BF16, F16])
+@pytest.mark.parametrize("T,D", [(3, 64), (2100, 128)])
+def test_no_rotation_leaves_values_alone(pkg, act, T, D):
+    """rope_theta 0 and no norm: queries and keys as they are, infinities and NaN in one half without influence on the other."""
+    g = torch.Generator(device="cuda").manual_seed(61)
+    q, k, v = (torch.randn(T, h, D, generator=g, device="cuda").to(act) for h in (4, 2, 2))
+    for t in (q, k):
+        t[0, 0, 3], t[1, 1, D // 2 + 5], t[2, 0, 1], t[T - 1, 1, D - 1] = math.inf, -math.inf, math.nan, math.inf
+    kc, vc = pool(T, 2, 1, D, act, "hnd")
+    at = torch.arange(T, device="cuda").int()
+    got = pkg.paged_append(q, k, v, at + 1000, at, kc, vc, rope_theta=0.0)
+    for x, y in ((got, q), (kc[:, :, 0], k), (vc[:, :, 0], v)):
+        assert torch.equal(torch.isnan(x), torch.isnan(y)) and torch.equal(torch.nan_to_num(x, nan=7.0), torch.nan_to_num(y, nan=7.0))

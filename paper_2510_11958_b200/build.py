@@ -27,11 +27,25 @@ def _stale(made, deps) -> bool:
     return any(os.path.getmtime(d) > t for d in deps if os.path.exists(d))
 
 
+def _made_for() -> str:
+    """What the binding is compiled against besides the sources: it uses torch's C++ interface and carries no tag in its name."""
+    import torch
+    return f"torch {torch.__version__}, {sysconfig.get_config_var('SOABI')}"
+
+
+def _binding_stale() -> bool:
+    if _stale(BINDING, ["paged_binding.cpp"]):
+        return True
+    with open(BINDING, "rb") as f:
+        return b"[made for " + _made_for().encode() + b"]" not in f.read()
+
+
 def _binding_command(to):
     import torch
     from torch.utils import cpp_extension
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + sysconfig.get_paths()["include"], "-I/usr/local/cuda/include"]
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + sysconfig.get_paths()["include"], "-I/usr/local/cuda/include",
+           f'-DDMTD_MADE_FOR="[made for {_made_for()}]"']
     cmd += ["-isystem" + p for p in cpp_extension.include_paths()]
     cmd += [os.path.join(HERE, "csrc", "paged_binding.cpp"), "-o", to]
     for p in cpp_extension.library_paths():
@@ -42,7 +56,7 @@ def _binding_command(to):
 def build(force: bool = False, verbose: bool = False) -> str:
     if force or _stale(LIB, SOURCES + HEADERS):
         _build_library(verbose)
-    if force or _stale(BINDING, ["paged_binding.cpp"]):
+    if force or _binding_stale():
         tmp = BINDING + f".tmp{os.getpid()}"
         _run(_binding_command(tmp), verbose)
         os.replace(tmp, BINDING)

@@ -186,7 +186,8 @@ PyMethodDef methods[] = {
     {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(append)), METH_FASTCALL, nullptr},
     {"attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(attention)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+// (the text is what build.py looks for in the file: the versions of torch and Python that it was compiled against)
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged", "Argument marshalling of the paged cache's calls " DMTD_MADE_FOR, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

@@ -127,3 +127,12 @@ def test_tensors_off_the_device_are_refused(dll):
         binding._paged().plan(i)
     with pytest.raises(ValueError, match="is no tensor"):
         binding._paged().attention(*[None] * 9)
+
+
+def test_the_binding_is_built_anew_for_another_torch(dll, monkeypatch):
+    import torch
+    from paper_2510_11958_b200 import binding, build
+    assert not build._binding_stale()
+    assert torch.__version__ in binding._paged().__doc__
+    monkeypatch.setattr(torch, "__version__", torch.__version__ + "1")
+    assert build._binding_stale()

@@ -294,7 +294,10 @@ dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32
  *   row_start [n_requests + 1], rising; lens [n_requests]: keys, the new rows' own among them (which
  *                             are in the cache already); table [n_requests][table_stride]
  *   max_new                   the most new rows of a request as far as the host knows, 0 = unknown.
- *                             Chooses between forms of the kernels; results do not hang on it
+ *                             Chooses between forms of the kernels, never what is computed: too small
+ *                             a number costs time, not rows.  With 16-bit queries the forms round
+ *                             probabilities differently (below), so that the bits are the same from call to
+ *                             call only with the same max_new; with 1 all requests take the finer form
  *   scratch                   device memory of at least DMTD_PAGED_ATTENTION_SCRATCH_BYTES bytes,
  *                             16-byte aligned, owned by the caller; holds partial results while the call's
  *                             kernels run (calls sharing one scratch must be stream-ordered, captured
@@ -302,9 +305,10 @@ dmtd_status dmtd_paged_append(const void *q, const void *k, const void *v, int32
  *   out [n_rows][n_q_heads][head_dim]   in q_dtype; overlaps no other array.  Rows of no request
  *                             are left as they were
  * Types: fp32 queries with any cache (results to fp32 accuracy: queries and probabilities enter
- * the tensor cores in two or three parts), or 16-bit queries with a cache of the same type (in requests
- * with some dozens of query rows to a kv head the probabilities are rounded once to that type before the
- * product with V, in others they enter it in two parts).  Sums and maxima are fp32.  A row that sees no key (a length below
+ * the tensor cores in two or three parts), or 16-bit queries with a cache of the same type (probabilities
+ * enter the product with V in two parts of that type; in requests with more than 32 query rows to a kv
+ * head, 48 with head_dim 64, if max_new admits such, they are rounded to it once: a result is then off by up to
+ * half a step of sum p |v| more).  Sums and maxima are fp32.  A row that sees no key (a length below
  * its rows, pages outside the pool, which take their keys out), or none whose weight is not zero, gives zeros.
  * Keys and values of positions that a row does not see have no influence on it, whatever they hold.
  * Errors: SHAPE for head_dim not 64/128, n_q_heads % n_kv_heads != 0 or more than 16 query heads per

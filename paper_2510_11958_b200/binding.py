@@ -414,7 +414,8 @@ def paged_attention(q, row_start, lens, table, k_cache, v_cache, max_new=0, scra
 
     q: cuda [T, nq, D], float32 with any cache or of the cache's 16-bit type, rows any multiple of 16 bytes apart; row_start:
     cuda int32 [B + 1], lens: cuda int32 [B] with the new rows counted, table: cuda int32 [B, pages] (PagedPlan); k_cache,
-    v_cache as in paged_append.  Rows of no request are left as they were in `out` (allocated if not given).
+    v_cache as in paged_append.  max_new: the most new rows of a request as far as the caller knows, 0 = unknown (time hangs on it
+    and, with 16-bit queries, how probabilities are rounded).  Rows of no request are left as they were in `out` (allocated if not given).
     `scratch`: a cuda tensor of PAGED_ATTENTION_SCRATCH_BYTES bytes or more, allocated through torch if not given.
     """
     if scratch is None:

@@ -218,3 +218,23 @@ def test_no_rotation_leaves_values_alone(pkg, act, T, D):
     got = pkg.paged_append(q, k, v, at + 1000, at, kc, vc, rope_theta=0.0)
     for x, y in ((got, q), (kc[:, :, 0], k), (vc[:, :, 0], v)):
         assert torch.equal(torch.isnan(x), torch.isnan(y)) and torch.equal(torch.nan_to_num(x, nan=7.0), torch.nan_to_num(y, nan=7.0))
+
+
+# ---- the forms that max_new chooses between
+
+@pytest.mark.parametrize("qt", [BF16, F16])
+@pytest.mark.parametrize("nq,nkv,D,cached,new", [(8, 2, 128, [700, 30], [300, 9]), (8, 8, 64, [0, 2500], [49, 120]), (16, 1, 128, [90], [3])])
+def test_what_max_new_may_change(pkg, qt, nq, nkv, D, cached, new):
+    """max_new 1: probabilities in two parts, each off by half a step of its own (a step of the first part squared: 2^-16, 2^-22).  Unknown:
+    once rounded in the larger requests, half a step of sum p |v| further.  Both: the result's own rounding, and 2e-5 of sum p |v| as everywhere."""
+    c = attention_case(71, cached, new, nq, nkv, D, qt, qt, 16, "hnd")
+    ref, size = attention_reference(c["q"], c["start"], c["lens"], c["table"], c["kc"], c["vc"], c["out"])
+    args = c["q"], ints(c["start"]), ints(c["lens"]), c["table"], c["kc"], c["vc"]
+    fine, coarse = (pkg.paged_attention(*args, max_new=m) for m in (1, 0))
+    h = half_step(qt)
+    # fp16: parts below 2^-24 of a probability of 2^8 or more, for as many keys as there are; results below 2^-14
+    base = (2e-5 + h * h) * size + 1e-6 + (max(c["lens"]) * 2.0 ** -33 * c["vc"].nan_to_num(0).abs().max() + 2.0 ** -25 if qt == F16 else 0)
+    assert ((fine.double() - ref).abs() <= h * ref.abs() + base).all()
+    assert ((coarse.double() - ref).abs() <= h * (ref.abs() + size) + base).all()
+    for m, want in ((1, fine), (0, coarse), (max(new), coarse)):
+        assert torch.equal(pkg.paged_attention(*args, max_new=m), want)

@@ -4,7 +4,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_paged import BF16, F16, F32, TYPES, attention_case, attention_reference, check_attention, half_step, ints, pkg, pool  # noqa: F401
+from test_gpu_paged import BF16, F16, F32, TYPES, attention_case, attention_reference, check_attention, half_step, ints, pkg, plan_case, plan_reference, \
+    pool  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -238,3 +239,47 @@ def test_what_max_new_may_change(pkg, qt, nq, nkv, D, cached, new):
     assert ((coarse.double() - ref).abs() <= h * (ref.abs() + size) + base).all()
     for m, want in ((1, fine), (0, coarse), (max(new), coarse)):
         assert torch.equal(pkg.paged_attention(*args, max_new=m), want)
+
+
+# ---- both sides of every border between launch shapes
+
+@pytest.mark.parametrize("B,page,width,most_new,n_rows,ended", [
+    (7, 16, 20, 60, 512, 0.2), (7, 16, 20, 60, 513, 0.2),                   # a block of 128 threads, of 512
+    (128, 16, 8, 3, 500, 0.1), (129, 16, 8, 3, 500, 0.1),
+    (512, 16, 8, 1, 1000, 0.1), (513, 16, 8, 1, 1000, 0.1),                 # of 512, of 1024
+    (7, 16, 20, 100, 1024, 0.2), (7, 16, 20, 100, 1025, 0.2),               # a block, a cluster
+    (1024, 16, 8, 0, 1024, 0.1), (1025, 16, 8, 0, 1024, 0.1),
+    (60, 32, 30, 400, 16384, 0.1), (60, 32, 30, 400, 16385, 0.1),           # rows by the same launch, by a second one
+])
+def test_plan_at_the_borders(pkg, B, page, width, most_new, n_rows, ended):
+    for seed in range(2):
+        lens, n_new, table, stack, n_pages, rows = plan_case(seed, B, page, width, most_new, 0, seed == 1, ended, seed == 1)
+        want = plan_reference(lens, n_new, table, stack, n_pages, page, n_rows)          # (rows behind the last request's, or too few of them)
+        free = torch.full((n_pages,), -9, dtype=torch.int32, device="cuda")
+        free[:len(stack)] = ints(stack)
+        t = ints(table)
+        p = pkg.paged_plan(ints(lens), ints(n_new), t, free, ints([len(stack)]), page, n_rows)
+        for name, got, ref in zip(p._fields, p, want):
+            assert got.tolist() == list(ref), (seed, name)
+        assert t.tolist() == want[-1], seed
+
+
+@pytest.mark.parametrize("T", [1, 2, 166, 167, 200, 222, 223, 250, 285, 286, 333, 334, 400, 401, 500, 501, 666, 667, 1000, 1001, 2000, 2001])
+@pytest.mark.parametrize("nq,nkv,D,act", [(32, 8, 128, BF16), (4, 2, 64, F32), (5, 1, 64, F16), (0, 1, 128, F32)])
+def test_append_parts_of_a_row(pkg, nq, nkv, D, act, T):
+    """Rows cut into 2000 / T parts: every part's vectors once, whatever the number of parts; as the rows one by one give them."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    q, k, v = (torch.randn(T, h, D, generator=g, device="cuda").to(act) if h else None for h in (nq, nkv, nkv))
+    pos = torch.randint(0, 1 << 16, (T,), generator=g, device="cuda").int()
+    slot = torch.randperm(T, generator=g, device="cuda").int()
+    norm = 1 + 0.1 * torch.randn(D, generator=g, device="cuda")
+    kc, vc = pool(T, nkv, 1, D, act, "hnd", fill=9.0)
+    got = pkg.paged_append(q, k, v, pos, slot, kc, vc, q_norm=norm, k_norm=norm, rope_theta=1e6)
+    some = sorted({0, T // 3, T - 1})
+    for t in some:
+        one = slice(t, t + 1)
+        k1, v1 = pool(T, nkv, 1, D, act, "hnd")
+        q1 = pkg.paged_append(None if q is None else q[one], k[one], v[one], pos[one], slot[one], k1, v1, q_norm=norm, k_norm=norm, rope_theta=1e6)
+        at = slot[t].long()
+        assert torch.equal(kc[at], k1[at]) and torch.equal(vc[at], v1[at]) and (q is None or torch.equal(got[t], q1[0]))
+    assert torch.equal(vc[slot.long(), :, 0], v) and not (kc == 9.0).all(-1).any()

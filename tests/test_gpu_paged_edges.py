@@ -283,3 +283,130 @@ def test_append_parts_of_a_row(pkg, nq, nkv, D, act, T):
         at = slot[t].long()
         assert torch.equal(kc[at], k1[at]) and torch.equal(vc[at], v1[at]) and (q is None or torch.equal(got[t], q1[0]))
     assert torch.equal(vc[slot.long(), :, 0], v) and not (kc == 9.0).all(-1).any()
+
+
+# ---- calls that the header allows
+
+@pytest.mark.parametrize("qt,kv", TYPES)
+def test_rows_in_front_of_the_first_request(pkg, qt, kv):
+    """row_start need not begin at 0: rows of no request, in front and behind, stay as they were."""
+    c = attention_case(81, [100, 0, 900], [70, 3, 1], 8, 2, 128, qt, kv, 16, "hnd", pad=9)
+    c["start"] = [s + 5 for s in c["start"]]
+    got = check_attention(pkg, c)
+    assert (got[:5] == 5.0).all() and (got[c["start"][-1]:] == 5.0).all()
+
+
+@pytest.mark.parametrize("qt,kv", TYPES)
+def test_requests_that_share_pages(pkg, qt, kv):
+    """A prompt's common pages in several tables, twice in one; other lengths behind them."""
+    c = attention_case(82, [96, 30, 64, 5], [40, 2, 1, 3], 8, 2, 64, qt, kv, 16, "nhd")
+    first = c["table"][0, :6].clone()
+    c["table"][1, :1] = first[0]
+    c["table"][2, :4] = first[:4]
+    c["table"][0, 5] = first[0]
+    c["table"][3, 0] = first[2]
+    check_attention(pkg, c)
+
+
+@pytest.mark.parametrize("qt,kv", [(F32, F16), (BF16, BF16)])
+def test_the_most_requests(pkg, qt, kv):
+    B = 8192
+    cached = [7 * b % 40 for b in range(B)]
+    new = [b % 3 for b in range(B)]
+    new[5000], new[8191] = 80, 40
+    # keys and values at once: a page to 64 positions, requests one after the other
+    g = torch.Generator(device="cuda").manual_seed(83)
+    page, nq, nkv, D = 64, 2, 1, 64
+    lens = [a + n for a, n in zip(cached, new)]
+    held = torch.tensor([-(-n // page) for n in lens])
+    width = int(held.max())
+    table = torch.full((B, width), -1, dtype=torch.int32)
+    col = torch.arange(width)[None] < held[:, None]
+    table[col] = torch.randperm(int(held.sum()), generator=torch.Generator().manual_seed(1)).int()
+    kc, vc = (torch.randn(int(held.sum()), nkv, page, D, generator=g, device="cuda").to(kv) for _ in range(2))
+    start = [0]
+    for n in new:
+        start.append(start[-1] + n)
+    q = torch.randn(start[-1], nq, D, generator=g, device="cuda").to(qt)
+    args = ints(start), ints(lens), table.cuda(), kc, vc
+    got = pkg.paged_attention(q, *args)
+    # every request by itself
+    for b in (1, 2, 31, 32, 4097, 4999, 5000, 5002, 8190, 8191):
+        if new[b]:
+            one = pkg.paged_attention(q[start[b]:start[b + 1]], ints([0, new[b]]), ints([lens[b]]), args[2][b:b + 1], kc, vc)
+            assert (got[start[b]:start[b + 1]].float() - one.float()).abs().max() <= 4 * half_step(qt) * one.float().abs().max() + 1e-5
+    dense = {n: [b for b in range(B) if new[b] == 1 and lens[b] == n] for n in (1, 20, 40)}
+    for n, some in dense.items():
+        at = args[2][some, 0].long()
+        p = torch.softmax(torch.einsum("bhd,bkd->bhk", q[[start[b] for b in some]].double(), kc[at, 0, :n].double()) / 8.0, -1)
+        ref = torch.einsum("bhk,bkd->bhd", p, vc[at, 0, :n].double())
+        assert ((got[[start[b] for b in some]].double() - ref).abs() <= 2 * half_step(qt) * vc.float().abs().max() + 2e-5).all()
+
+
+@pytest.mark.parametrize("qt,kv", TYPES)
+@pytest.mark.parametrize("nq,nkv,D,page,cached,new", [
+    (64, 64, 64, 16, [40, 3], [50, 1]),                              # many kv heads
+    (7, 7, 128, 2, [10, 90], [34, 3]),                               # pages smaller than a copy
+    (8, 8, 128, 32, [0, 333], [700, 41]),                            # one query head to a kv head, several row tiles
+    (16, 16, 64, 4096, [900], [260]),                                # a page for all
+    (48, 3, 64, 8, [17], [33]),
+])
+def test_other_head_counts(pkg, qt, kv, nq, nkv, D, page, cached, new):
+    c = attention_case(84, cached, new, nq, nkv, D, qt, kv, page, "hnd", pad=1)
+    for max_new in (0, 1):
+        check_attention(pkg, c, max_new=max_new)
+
+
+def test_two_graphs_take_turns_on_one_scratch(pkg):
+    cases = [attention_case(85, [900, 4], [200, 1], 8, 2, 128, BF16, BF16, 16, "hnd"), attention_case(86, [0, 1300, 60], [90, 1, 40], 8, 8, 64, F16, F16, 32, "nhd")]
+    want = [check_attention(pkg, c) for c in cases]
+    args = [(c["q"], ints(c["start"]), ints(c["lens"]), c["table"], c["kc"], c["vc"]) for c in cases]
+    scratch = torch.empty(pkg.PAGED_ATTENTION_SCRATCH_BYTES, dtype=torch.uint8, device="cuda")
+    outs = [torch.zeros_like(c["out"]) for c in cases]
+    graphs = []
+    for a, o in zip(args, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(3):
+                pkg.paged_attention(*a, scratch=scratch, out=o)
+        graphs.append(g)
+    for _ in range(10):
+        for g, o in zip(graphs, outs):
+            o.fill_(5.0)
+            g.replay()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+_FIRST_CALL = """
+import torch
+import paper_2510_11958_b200 as pkg
+ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+q, k, v = (torch.randn(120, h, 64, device="cuda").bfloat16() for h in (4, 2, 2))
+kc, vc = (torch.zeros(10, 2, 16, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+lens, n_new, table, free, n_free = ints([0, 0]), ints([119, 1]), ints([[-1] * 8] * 2), torch.arange(10, device="cuda").int(), ints([10])
+torch.cuda.synchronize()
+def step():
+    p = pkg.paged_plan(lens, n_new, table, free, n_free, 16, 120)
+    r = pkg.paged_append(q, k, v, p.position, p.slot, kc, vc, rope_theta=1e4)
+    return p, r, pkg.paged_attention(r, p.row_start, p.lens, table, kc, vc)
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    p, r, out = step()
+g.replay()
+torch.cuda.synchronize()
+assert p.lens.tolist() == [119, 1] and torch.isfinite(out).all()
+first = out.clone()
+free.copy_(torch.arange(10, device="cuda").int())
+p, r, out = step()
+assert torch.equal(out, first)
+print("fine")
+"""
+
+
+def test_the_first_calls_of_a_process_are_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", _FIRST_CALL], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stdout + r.stderr

@@ -15,24 +15,25 @@
 
 namespace dmtd {
 
-// Sum of floor((a i + b) / m) over i = 0 .. n - 1, by exchanging the roles of i and the quotient (a lattice-point
-// count under a line, as in Euclid's algorithm).
-__host__ __device__ __forceinline__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned long long b) {
-  long long s = 0;
-  for (;;) {
-    if (a >= m) { s += (long long)n * (n - 1) / 2 * (a / m); a %= m; }
-    if (b >= m) {
-      const unsigned long long q = b >> 32 ? b / m : (unsigned)b / m;
-      s += (long long)(n * q);
-      b -= q * m;
-    }
-    const unsigned long long y = (unsigned long long)a * n + b;
-    if (y < m) return s;
-    const unsigned long long q = y >> 32 ? y / m : (unsigned)y / m;
-    b = y - q * m;
-    n = (unsigned)q;
-    const unsigned t = m; m = a; a = t;
+// Sum of floor((a i + b) / m) over i = 0 .. n - 1, for a, b < m and a n + b < 2^32.  It counts the points (i, j) with j >= 1 and
+// j m <= a i + b; column by column instead of row by row these are n - ceil((j m - b) / a) for every j up to the last row's quotient, so
+// that n q minus a sum of the same kind with a and m exchanged remains (the reciprocity of such sums: Graham, Knuth, Patashnik, Concrete
+// Mathematics, section 3.5), a step of Euclid's algorithm at a time.
+__host__ __device__ __forceinline__ long long quotients_sum(unsigned n, unsigned a, unsigned b, unsigned m) {
+  long long sum = 0, sign = 1;
+  while (n > 0 && a > 0) {
+    const unsigned q = (a * (n - 1) + b) / m;
+    sum += sign * (long long)n * q;
+    // ceil((j m - b) / a), j = 1 .. q, is floor((m j' + m - b + a - 1) / a), j' = 0 .. q - 1; whole parts go to the sum at once
+    const unsigned rest = m - b + a - 1, slope = m % a;
+    sum -= sign * ((long long)(m / a) * q * (q - 1ll) / 2 + (long long)(rest / a) * q);
+    sign = -sign;
+    m = a;
+    a = slope;
+    b = rest % m;
+    n = q;
   }
+  return sum;
 }
 
 // x / y without the 64-bit division where 32 bits do
@@ -69,7 +70,7 @@ struct PagedRequest {
     const unsigned long long base = (unsigned long long)((long long)c + (none + 1ll) * K.tile) + unit - 1;
     if (n_sum == 0) {
     } else if (K.lg_tile < 0) {
-      s += floor_sum(n_sum, unit, K.tile, base);
+      s += (long long)(base >> lg) * n_sum + quotients_sum(n_sum, K.tile, (unsigned)(base & (unit - 1)), unit);         // (tile < unit: 3 heads or more)
     } else if (K.lg_tile >= (int)lg) {
       s += (long long)(base >> lg) * n_sum + ((long long)n_sum * (n_sum - 1) / 2 << (K.lg_tile - lg));
     } else {
@@ -370,8 +371,8 @@ __device__ __forceinline__ void paged_join_rows(const PagedAttentionParams &P, c
 }
 
 // Joins what was cut: a block to each of the row kernel's `blocks` shares, a warp to a row; then, if the chunk kernel ran
-// too, per_chunk blocks to each of its shares.  Bound: two trips to memory, 3 to 4.5 us; behind the chunk kernel the partial results (35 MB, most of
-// them still in L2), 8 us.
+// too, per_chunk blocks to each of its shares.  Bound: two trips to memory, 3 to 4.5 us; behind the chunk kernel the partial results (35 MB), 8 us
+// where most of them are still in L2 and 14 with cold caches.
 constexpr int PAGED_MERGE_WARPS = 16;
 template <int D> __host__ __device__ constexpr int paged_merge_per_chunk(int rows) { return rows / 32 * (D / 16) / PAGED_MERGE_WARPS; }
 template <typename T, typename KVT, int D>

@@ -8,9 +8,10 @@
 // cores' least, 2560 with N = 64, which reads Q twice as often.)  Each half has an issuing warp of its own: an MMA takes a warp some 70
 // cycles to issue, and one warp for both halves was the bound of it all (6130 cycles).
 //
-// Measured: 2000 rows over 8000 keys, 32 query heads on 8, head_dim 128, pages of 16: 233 us as a graph, with the merge, 985 TFLOP/s.  A step takes
+// Measured: 2000 rows over 8000 keys, 32 query heads on 8, head_dim 128, pages of 16: 258 us with the merge, 890 TFLOP/s, call after call or as a graph,
+// at the 1.78 GHz that the power cap leaves; 233 us in the first milliseconds, at the full clock, which is what the figures of other forms here stand beside.  A step takes
 // 2250 cycles: a softmax warp 510 for S and its maximum, 1200 for exponentials and P (800 while the other half's warps have none), 300 for its two
-// barriers; an issuing warp's turn takes 1900.  (Freeing S when it is in registers, with P beside it: 254 us; two threads to a row: 262 to 274.)
+// barriers; an issuing warp's turn takes 1900.  (Freeing S when it is in registers, with P beside it: 254 us against 233; two threads to a row: 262 to 274.)
 //
 // As in the row kernel a row's reference is raised only when a score lies more than 2^6 above it; then O is read
 // back and scaled.

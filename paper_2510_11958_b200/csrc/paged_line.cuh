@@ -19,7 +19,8 @@ namespace dmtd {
 // j m <= a i + b; column by column instead of row by row these are n - ceil((j m - b) / a) for every j up to the last row's quotient, so
 // that n q minus a sum of the same kind with a and m exchanged remains (the reciprocity of such sums: Graham, Knuth, Patashnik, Concrete
 // Mathematics, section 3.5), a step of Euclid's algorithm at a time.
-__host__ __device__ __forceinline__ long long quotients_sum(unsigned n, unsigned a, unsigned b, unsigned m) {
+// (Not inlined: the chunk kernel, which hardly calls it, takes 258 us instead of 263 for 2000 rows over 8000 keys.)
+__host__ __device__ __noinline__ inline long long quotients_sum(unsigned n, unsigned a, unsigned b, unsigned m) {
   long long sum = 0, sign = 1;
   while (n > 0 && a > 0) {
     const unsigned q = (a * (n - 1) + b) / m;
@@ -259,7 +260,7 @@ struct PagedScratch {
 // The row kernel behind a chunk kernel starts while that one runs.  griddepcontrol.wait alone would make what the launches in front of both have
 // written (lengths, tables, queries, the cache's new rows) visible to it, and only at the chunk kernel's end.  So a thread of the
 // chunk kernel that has waited releases this word before it lets the row kernel in, the row kernel's blocks acquire it, and
-// the merge clears it.  A block that does not find it waits for the chunk kernel's end.  (Waiting always: 144 us instead of 136 for the rows
+// its first block clears it at its end (in the merge that costs 0.7 us a call).  A block that does not find it waits for the chunk kernel's end.  (Waiting always: 144 us instead of 136 for the rows
 // and pieces of `attention_mixed`; the row kernel in front: 141.)
 constexpr unsigned PAGED_ENTERED = 0x9d1c6b35u;
 __device__ __forceinline__ bool paged_entered(const unsigned *entered) {
@@ -380,7 +381,6 @@ __global__ void __launch_bounds__(PAGED_MERGE_WARPS * 32) paged_merge_kernel(con
                                                                               PagedScratch S_chunk) {
   paged_enter();
   const int warp = threadIdx.x >> 5, G = P.nq / P.nkv;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *S_chunk.entered = 0;
   if ((int)blockIdx.x < blocks) {
     const PagedCutItem c = S.items[blockIdx.x];
     if (c.pieces && warp < c.rows * G) paged_join_row<T, KVT, D>(P, S, c, blockIdx.x, warp);

@@ -346,12 +346,18 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
   // Behind the chunk kernel this one reads nothing that that kernel writes: it acquires what lies in front of both (paged_line.cuh) and
   // waits at its end, for the grids behind it.
   auto wait = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
+  auto leave = [&] {
+    if (!behind_chunk) return;
+    wait();
+    // (a block that comes later waits for the chunk kernel, which has ended)
+    if (blockIdx.x == 0 && threadIdx.x == 0) *S.entered = 0;
+  };
   if (!behind_chunk || !__syncthreads_or(threadIdx.x == 0 && paged_entered(S.entered))) wait();
   RowsShare share;
   share.plan(P, K, sh.line, blockIdx.x, gridDim.x);
   if (share.begin >= share.end) {
     if (threadIdx.x == 0) S.items[blockIdx.x].pieces = 0;
-    if (behind_chunk) wait();
+    leave();
     return;
   }
   // thread 0 keeps the list of pieces five ahead, so that what a piece looks at was made before a barrier
@@ -607,14 +613,12 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
 #pragma unroll
       for (int w = 0; w < PR_WARPS; ++w) {
         const float mw = red_m[w * PR_ROWS + qi];
-        if (mw == -INFINITY) {
-          l += red_l[w * PR_ROWS + qi];                        // a warp without keys: 0; one whose scores are all NaN: NaN
-        } else {
-          const float f = exp2_approx(mw - m);
-          const float4 v = *reinterpret_cast<const float4 *>(o_s + (w * PR_ROWS + qi) * C::OROW + at);
-          l = fmaf(red_l[w * PR_ROWS + qi], f, l);
-          acc[0] = fmaf(v.x, f, acc[0]); acc[1] = fmaf(v.y, f, acc[1]); acc[2] = fmaf(v.z, f, acc[2]); acc[3] = fmaf(v.w, f, acc[3]);
-        }
+        // a warp without keys has sum 0, one whose scores are all NaN sum NaN, which stays (a branch around the first: 43.5 us instead of
+        // 41.2 for 32 requests of three rows)
+        const float f = mw > -INFINITY ? exp2_approx(mw - m) : 0.f;
+        const float4 v = *reinterpret_cast<const float4 *>(o_s + (w * PR_ROWS + qi) * C::OROW + at);
+        l = fmaf(red_l[w * PR_ROWS + qi], f, l);
+        acc[0] = fmaf(v.x, f, acc[0]); acc[1] = fmaf(v.y, f, acc[1]); acc[2] = fmaf(v.z, f, acc[2]); acc[3] = fmaf(v.w, f, acc[3]);
       }
       if (whole) {
         const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -643,7 +647,7 @@ __global__ void __launch_bounds__(PR_THREADS, 2) paged_rows_kernel(const __grid_
     }
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
-  if (behind_chunk) wait();
+  leave();
 }
 
 }  // namespace dmtd

@@ -627,7 +627,12 @@ __global__ void __launch_bounds__(PC_THREADS, 1) paged_chunk_kernel(const __grid
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(PC_TMEM) : "memory");
+  if (warp == 8) {
+    // Tensor memory is not given back under an MMA.  At a share's end none is left; those that a block had issued when a wait gave up
+    // take some microseconds, whatever the wait was for: they get 100.  (A commit and a wait for it: 263 us instead of 260.)
+    for (int i = 0; i < 100 * sh.gave_up; ++i) __nanosleep(1000);
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(PC_TMEM) : "memory");
+  }
   if (work && (sh.again || sh.gave_up)) chunk_again<T, D>(P, K, S, sh);
 }
 

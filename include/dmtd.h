@@ -215,6 +215,8 @@ dmtd_status dmtd_attention_decode_static(const float *q, const void *k, const vo
  *
  * (the paper's cyclical refilling, Section 2.2, with requests of their own lengths: one to tau new
  * rows each, or a piece of a prompt).  (The paper has no counterpart: it measures static batches.)
+ * Inside a cycle the lower layers' cache is behind the upper layers': each kind has lengths, a table,
+ * free pages and pools of its own, and a plan over them (tau rows in a cycle's full pass; one in every pass).
  * Lengths, tables and offsets are read on the device when the kernels run, so a captured graph of
  * a step stays valid while requests grow.  Values in them that do not fit the buffers are cut off: lengths
  * to [0, table_stride * page_size], row offsets to [0, n_rows]; slots and pages outside the

@@ -410,3 +410,54 @@ def test_the_first_calls_of_a_process_are_captured():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", _FIRST_CALL], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "fine" in r.stdout, r.stdout + r.stderr
+
+
+# ---- a decode cycle with cyclical refilling: two plans over two tables
+
+@pytest.mark.parametrize("kv", [BF16, F16])
+def test_refill_cycles_over_two_plans(pkg, kv):
+    """Lower layers get all tokens of the cycle before at once, upper layers a token a pass: their lengths differ inside a cycle, so that each
+    kind has a plan, a table and a pool of its own.  Requests with prompts and cycles of their own; every pass against dense histories in fp64."""
+    g = torch.Generator(device="cuda").manual_seed(91)
+    B, nq, nkv, D, page, width = 4, 8, 2, 64, 8, 12
+    tau, prompt = [3, 1, 4, 2], [40, 1, 17, 8]
+
+    class Stack:
+        def __init__(self, n_pages):
+            self.lens, self.n_free = ints([0] * B), ints([n_pages])
+            self.table = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+            self.free = torch.randperm(n_pages, generator=g, device="cuda").int()
+            self.kc, self.vc = pool(n_pages, nkv, page, D, kv, "nhd", fill=float("nan"))
+            self.past = [[torch.zeros(0, nkv, D, dtype=kv, device="cuda") for _ in range(2)] for _ in range(B)]
+
+        def step(self, new):
+            """New rows of every request through one layer: plan, append (no rotation: the history is what was given), attention."""
+            T = sum(new)
+            q, k, v = (torch.randn(T, h, D, generator=g, device="cuda").to(kv) for h in (nq, nkv, nkv))
+            p = pkg.paged_plan(self.lens, ints(new), self.table, self.free, self.n_free, page, T)
+            assert p.granted.tolist() == new
+            q = pkg.paged_append(q, k, v, p.position, p.slot, self.kc, self.vc)
+            out = pkg.paged_attention(q, p.row_start, p.lens, self.table, self.kc, self.vc, max_new=max(new))
+            self.lens, self.n_free = p.lens, p.n_free
+            at = 0
+            for b, n in enumerate(new):
+                rows = slice(at, at + n)
+                at += n
+                self.past[b] = [torch.cat([old, x[rows]]) for old, x in zip(self.past[b], (k, v))]
+                kb, vb = (x.double().repeat_interleave(nq // nkv, 1) for x in self.past[b])
+                s = torch.einsum("rhd,khd->hrk", q[rows].double(), kb) / math.sqrt(D)
+                w = torch.softmax(s + torch.full_like(s, -math.inf).triu(len(kb) - n + 1), -1)
+                ref, size = torch.einsum("hrk,khd->rhd", w, vb), torch.einsum("hrk,khd->rhd", w, vb.abs())
+                # probabilities and result rounded once each, as in the other tests
+                assert ((out[rows].double() - ref).abs() <= half_step(kv) * (size + ref.abs()) + 2e-5 * size + 1e-5).all()
+                assert p.lens[b].item() == len(kb)
+    lower, upper = Stack(B * width), Stack(B * width)
+    pending, done = list(prompt), [0] * B                             # tokens that the lower layers have not seen; passes of the cycle at hand
+    for n in range(9):
+        full = [done[b] % tau[b] == 0 for b in range(B)]
+        lower.step([pending[b] if full[b] else 0 for b in range(B)]) if any(full) else None
+        upper.step([prompt[b] if n == 0 else 1 for b in range(B)])    # the whole prompt in the first pass, then the newest token
+        pending = [1 if full[b] else pending[b] + 1 for b in range(B)]
+        done = [d + 1 for d in done]
+        for b in range(B):
+            assert upper.lens[b].item() - lower.lens[b].item() == (done[b] - 1) % tau[b]
